@@ -403,6 +403,87 @@ pq_status pq_decode_step_polar(const pq_ctx *ctx, const void *xk, const void *xv
                                void *hip_stream);
 
 /* ---------------------------------------------------------------------------
+ * Paged caches.  A page is a tile: page p of a head plane is its tile p, so a paged
+ * cache has the buffers of the others (codes, radii, pool_tokens = 64 * pages) and
+ * either kind of call may work on it.  A sequence owns pages in any order and
+ * anywhere: token t of sequence b lies in slot t & 63 of page
+ * pages[b * ld_pages + (t >> 6)], the same page of the key and of the value cache
+ * and of every head plane.  pages (device): int32, n_seq rows of ld_pages entries; an
+ * entry that is not in [0, pool_tokens / 64) names no page (-1, say, of tokens that
+ * have left a sliding window), and tokens from 64 * ld_pages on have none.  Tables,
+ * lengths and row numbers are read on the device.
+ *
+ * Ragged rows: row_start (device, int32 [n_seq + 1], non-decreasing from 0) says that
+ * rows row_start[b] .. row_start[b + 1] - 1 of a tensor are the newest tokens of
+ * sequence b, the last of them its token ctx_len[b] - 1 (ctx_len, device, int32
+ * [n_seq], counts them).  One token per sequence, chunks of prompts and both in one
+ * call are the same call.  Rows from row_start[n_seq] on (a padded batch) and rows
+ * whose token would be negative belong to no token.
+ *
+ * Position rotation: for p = position of a token, coordinates (i, i + dim / 2), or
+ * (2 i, 2 i + 1) if interleaved, i < dim / 2, become (x cos - y sin, x sin + y cos) with
+ * cos = cos_sin[p * dim + i] and sin = cos_sin[p * dim + dim / 2 + i]; coordinates from
+ * dim on stay.  cos_sin (device, fp32, 16-byte aligned): n_pos rows of dim, made by
+ * the caller, with any scaling of its angles; dim a multiple of 16, 128 at most
+ * (PQ_EUNSUPPORTED: another one).  Positions outside [0, n_pos) take the nearest row.
+ * NULL: no rotation.
+ * ------------------------------------------------------------------------- */
+typedef struct pq_rotary {
+    const float *cos_sin;
+    int64_t n_pos;
+    int dim;
+    int interleaved;
+} pq_rotary;
+
+/* Appends the keys and values of new tokens (ragged rows) to a paged cache; the keys
+ * are rotated to their tokens' positions on the way.  xk, xv (device): element
+ * (row, head, k) at [row * ld_token + head * ld_head + k], both with these strides,
+ * dtype xt, aligned as for pq_encode_kv (views of one projection's output may be
+ * passed as they are).  positions (device, int32 [n_rows]) or NULL: a token's place
+ * in its sequence.  A row whose page is none is not written.
+ * Codes are settled in 64 bits: a vector gets the codes of its definition -- products
+ * with S, rotation and cell comparisons in double precision where fewer bits leave
+ * them in doubt -- whatever batch it comes in (radii are within one rounding).
+ * Slots of a page that the call does not name keep their contents; two calls, or two
+ * sequences of one call, that write into one page must not overlap in time.
+ * n_rows * n_heads at most 2^30 - 1 (PQ_EUNSUPPORTED).  n_rows == 0 or n_seq == 0 is a
+ * no-op (pointers are not examined). */
+pq_status pq_append_paged(const pq_ctx *ctx, const void *xk, const void *xv, pq_dtype xt, int64_t n_rows, int n_heads,
+                          int64_t ld_token, int64_t ld_head, const pq_rotary *rotary, const int32_t *positions,
+                          uint8_t *k_codes, uint16_t *k_radii, uint8_t *v_codes, uint16_t *v_radii,
+                          int64_t pool_tokens, const int32_t *pages, int64_t ld_pages, const int32_t *row_start,
+                          const int32_t *ctx_len, int n_seq, void *hip_stream);
+
+/* DeQuant of ragged rows of a paged cache, keys to out_k and values to out_v (either may be
+ * NULL), as pq_decode_kv with rotated == 0: element (row, head, k) at
+ * [row * ld_token + head * ld_head + k], dtype ot.  With row_start = running sums of
+ * ctx_len whole sequences are read; with pq_append_paged's row_start what it wrote.
+ * Rows of a token whose page is none are zeros; rows that belong to no token keep
+ * their contents.  Keys come out as they are cached, rotated to their positions. */
+pq_status pq_decode_paged(const pq_ctx *ctx, const uint8_t *k_codes, const uint16_t *k_radii,
+                          const uint8_t *v_codes, const uint16_t *v_radii, int64_t pool_tokens,
+                          const int32_t *pages, int64_t ld_pages, const int32_t *row_start,
+                          const int32_t *ctx_len, int n_seq, int64_t n_rows, int n_heads,
+                          void *out_k, void *out_v, pq_dtype ot, int64_t ld_token, int64_t ld_head,
+                          void *hip_stream);
+
+/* pq_attn_decode_polar_mq (M == 1: pq_attn_decode_polar) on a paged cache: q, out [B][M][Hq][128],
+ * sequence b attends to its ctx_len[b] tokens in pages[b], query token m to the first
+ * ctx_len[b] - (M-1-m) of them.  rotary: q is rotated to the position of its token,
+ * positions[b * M + m] (device, int32) or, if positions is NULL, ctx_len[b] - M + m.
+ * Tokens of a page that is none take no part.  64 * ld_pages must be at least max_ctx
+ * (PQ_EINVAL).  workspace: pq_attn_paged_workspace_bytes, a smaller one as in
+ * pq_attn_decode_polar.  All else as there. */
+pq_status pq_attn_paged(const pq_ctx *ctx, const void *q, void *out, pq_dtype out_dtype, const pq_rotary *rotary,
+                        const int32_t *positions, const uint8_t *k_codes, const uint16_t *k_radii,
+                        const uint8_t *v_codes, const uint16_t *v_radii, int64_t pool_tokens,
+                        const int32_t *pages, int64_t ld_pages, const int32_t *ctx_len,
+                        int B, int M, int Hq, int Hkv, int64_t max_ctx, float softmax_scale,
+                        void *workspace, size_t workspace_bytes, void *hip_stream);
+
+size_t pq_attn_paged_workspace_bytes(int B, int M, int Hq, int Hkv, int64_t max_ctx);
+
+/* ---------------------------------------------------------------------------
  * Decode attention over a quantised prefix plus an unquantised recent window
  * (Section 5.3: the keys and values streamed in during generation are kept in
  * 16 bits, only the prompt's are quantised): one softmax over the DeQuant of

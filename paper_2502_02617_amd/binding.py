@@ -112,6 +112,15 @@ def library():
     L.pq_attn_decode_polar_static.restype = i32
     L.pq_attn_decode_polar_static.argtypes = [vp, vp, vp, i32, vp, vp, vp, vp, vp, vp, i32, i32, i32, i64, i64,
                                               ctypes.c_float, vp]
+    L.pq_append_paged.restype = i32
+    L.pq_append_paged.argtypes = [vp, vp, vp, i32, i64, i32, i64, i64, vp, vp, vp, vp, vp, vp, i64, vp, i64, vp, vp, i32, vp]
+    L.pq_decode_paged.restype = i32
+    L.pq_decode_paged.argtypes = [vp, vp, vp, vp, vp, i64, vp, i64, vp, vp, i32, i64, i32, vp, vp, i32, i64, i64, vp]
+    L.pq_attn_paged.restype = i32
+    L.pq_attn_paged.argtypes = [vp, vp, vp, i32, vp, vp, vp, vp, vp, vp, i64, vp, i64, vp, i32, i32, i32, i32, i64,
+                                ctypes.c_float, vp, ctypes.c_size_t, vp]
+    L.pq_attn_paged_workspace_bytes.restype = ctypes.c_size_t
+    L.pq_attn_paged_workspace_bytes.argtypes = [i32, i32, i32, i32, i64]
     L.pq_general_record_bytes.restype = ctypes.c_size_t
     L.pq_general_record_bytes.argtypes = [vp]
     L.pq_general_codebook_entries.restype = i32
@@ -182,6 +191,37 @@ def _dtype_code(t):
     if t.dtype == torch.float32:
         return PQ_F32
     raise PolarQuantError("only float32 and bfloat16 tensors are supported")
+
+
+class Rotary(ctypes.Structure):
+    """pq_rotary: position rotation by a table cos_sin, float32 device tensor [n_pos, dim], each row dim / 2 cosines, then dim / 2
+    sines; pairs (i, i + dim / 2), or (2 i, 2 i + 1) if interleaved.  Keeps the tensor alive."""
+    _fields_ = [("cos_sin", ctypes.c_void_p), ("n_pos", ctypes.c_int64), ("dim", ctypes.c_int), ("interleaved", ctypes.c_int)]
+
+    def __init__(self, cos_sin, interleaved=False):
+        import torch
+
+        super().__init__()
+        if cos_sin.dtype != torch.float32 or cos_sin.dim() != 2 or not cos_sin.is_contiguous() or not cos_sin.is_cuda:
+            raise PolarQuantError("cos_sin must be a contiguous float32 device tensor [n_pos, dim]")
+        self.tensor = cos_sin
+        self.cos_sin, self.n_pos, self.dim, self.interleaved = cos_sin.data_ptr(), cos_sin.shape[0], cos_sin.shape[1], int(bool(interleaved))
+
+
+def _ints(name, t, shape):
+    """Address of an int32 device tensor of that shape (a row of `pages` may be longer than it is read), rows contiguous."""
+    import torch
+
+    if t.dtype != torch.int32 or not t.is_cuda or tuple(t.shape) != tuple(shape) or (t.dim() and t.shape[-1] > 1 and t.stride(-1) != 1):
+        raise PolarQuantError(f"{name} must be an int32 device tensor of shape {list(shape)}, innermost dimension contiguous")
+    return t.data_ptr()
+
+
+def _pages(pages, n_seq):
+    if pages.dim() != 2:
+        raise PolarQuantError("pages must be [n_seq, pages per sequence]")
+    at = _ints("pages", pages, (n_seq, pages.shape[1]))
+    return at, int(pages.stride(0)) if n_seq > 1 else int(pages.shape[1])
 
 
 class Context:
@@ -486,6 +526,88 @@ class Context:
             win_v.data_ptr(), win_len.data_ptr(), int(win_k.shape[2]), int(B), int(Hq), int(Hkv), int(pool_tokens),
             int(max_ctx), float(softmax_scale), workspace.data_ptr(),
             int(workspace.numel() * workspace.element_size()), _stream()))
+
+    # ---- paged caches ----------------------------------------------------------
+    def _paged_cache(self, k_codes, k_radii, v_codes, v_radii):
+        """Checks the four buffers of a cache in this context's format -> (head planes, slots of a plane)."""
+        heads, tiles = k_codes.shape[0], k_codes.shape[1]
+        halves = self.radii_halves_per_tile()
+        for t, last in ((k_codes, TILE_CODE_BYTES), (v_codes, TILE_CODE_BYTES), (k_radii, halves), (v_radii, halves)):
+            if tuple(t.shape) != (heads, tiles, last) or not t.is_contiguous() or not t.is_cuda:
+                raise PolarQuantError("the cache must be as alloc_cache_for makes it, keys and values of one size")
+        return heads, tiles * TILE_TOKENS
+
+    def append_paged(self, xk, xv, row_start, ctx_len, k_codes, k_radii, v_codes, v_radii, pages, rotary=None, positions=None):
+        """xk, xv: [rows, n_heads, 128] of one shape, dtype and strides (views of a projection's output, say); row_start int32
+        [n_seq + 1], ctx_len int32 [n_seq] (new tokens counted), pages int32 [n_seq, pages]; rotary: Rotary for the keys, positions
+        int32 [rows] or None."""
+        if xk.dim() != 3 or xk.shape != xv.shape or xk.stride() != xv.stride() or xk.dtype != xv.dtype:
+            raise PolarQuantError("xk and xv must be [rows, n_heads, 128] of one shape, dtype and strides")
+        if xk.shape[2] != D or xk.stride(2) != 1 or not (xk.is_cuda and xv.is_cuda):
+            raise PolarQuantError("xk and xv must be device tensors with 128 contiguous coordinates")
+        heads, pool_tokens = self._paged_cache(k_codes, k_radii, v_codes, v_radii)
+        if xk.shape[1] != heads:
+            raise PolarQuantError("xk and the cache differ in heads")
+        n_seq = ctx_len.shape[0]
+        table, ld = _pages(pages, n_seq)
+        _check(library().pq_append_paged(
+            self._h, xk.data_ptr(), xv.data_ptr(), _dtype_code(xk), int(xk.shape[0]), heads, int(xk.stride(0)), int(xk.stride(1)),
+            ctypes.byref(rotary) if rotary is not None else None,
+            _ints("positions", positions, (xk.shape[0],)) if positions is not None else None,
+            k_codes.data_ptr(), k_radii.data_ptr(), v_codes.data_ptr(), v_radii.data_ptr(), pool_tokens, table, ld,
+            _ints("row_start", row_start, (n_seq + 1,)), _ints("ctx_len", ctx_len, (n_seq,)), int(n_seq), _stream()))
+
+    def decode_paged(self, k_codes, k_radii, v_codes, v_radii, pages, row_start, ctx_len, out_k=None, out_v=None):
+        """out_k, out_v: [rows, n_heads, 128] float32 or bfloat16, of one shape, dtype and strides, or one of them None."""
+        o = out_k if out_k is not None else out_v
+        if o is None:
+            raise PolarQuantError("give out_k, out_v or both")
+        for t in (out_k, out_v):
+            if t is not None and (t.dim() != 3 or t.shape != o.shape or t.stride() != o.stride() or t.dtype != o.dtype or t.shape[2] != D
+                                  or t.stride(2) != 1 or not t.is_cuda):
+                raise PolarQuantError("out_k and out_v must be [rows, n_heads, 128] device tensors of one shape, dtype and strides")
+        heads, pool_tokens = self._paged_cache(k_codes, k_radii, v_codes, v_radii)
+        if o.shape[1] != heads:
+            raise PolarQuantError("the outputs and the cache differ in heads")
+        n_seq = ctx_len.shape[0]
+        table, ld = _pages(pages, n_seq)
+        _check(library().pq_decode_paged(
+            self._h, k_codes.data_ptr(), k_radii.data_ptr(), v_codes.data_ptr(), v_radii.data_ptr(), pool_tokens, table, ld,
+            _ints("row_start", row_start, (n_seq + 1,)), _ints("ctx_len", ctx_len, (n_seq,)), int(n_seq), int(o.shape[0]), heads,
+            out_k.data_ptr() if out_k is not None else None, out_v.data_ptr() if out_v is not None else None, _dtype_code(o),
+            int(o.stride(0)), int(o.stride(1)), _stream()))
+
+    def attn_paged(self, q, out, k_codes, k_radii, v_codes, v_radii, pages, ctx_len, max_ctx, softmax_scale, workspace, rotary=None,
+                   positions=None):
+        """M query tokens per sequence on a paged cache: q, out [B, M, Hq, 128] (q bf16); ctx_len int32 [B], pages int32 [B, pages];
+        rotary: Rotary for the queries, positions int32 [B, M] or None."""
+        B, M, Hq = self._paged_queries(q, out)
+        heads, pool_tokens = self._paged_cache(k_codes, k_radii, v_codes, v_radii)
+        table, ld = _pages(pages, B)
+        _check(library().pq_attn_paged(
+            self._h, q.data_ptr(), out.data_ptr(), _dtype_code(out), ctypes.byref(rotary) if rotary is not None else None,
+            self._query_positions(positions, B, M), k_codes.data_ptr(), k_radii.data_ptr(), v_codes.data_ptr(), v_radii.data_ptr(),
+            pool_tokens, table, ld, _ints("ctx_len", ctx_len, (B,)), B, M, Hq, heads, int(max_ctx), float(softmax_scale),
+            workspace.data_ptr(), int(workspace.numel() * workspace.element_size()), _stream()))
+
+    @staticmethod
+    def _paged_queries(q, out):
+        if q.dim() != 4 or q.shape[3] != D or q.shape != out.shape or not (q.is_contiguous() and out.is_contiguous()) or \
+                _dtype_code(q) != PQ_BF16 or not (q.is_cuda and out.is_cuda):
+            raise PolarQuantError("q and out must be contiguous device tensors [B, M, Hq, 128], q bfloat16")
+        return int(q.shape[0]), int(q.shape[1]), int(q.shape[2])
+
+    @staticmethod
+    def _query_positions(positions, B, M):
+        if positions is None:
+            return None
+        if not positions.is_contiguous():
+            raise PolarQuantError("positions must be contiguous")
+        return _ints("positions", positions, (B, M))
+
+    @staticmethod
+    def attn_paged_workspace_bytes(B, M, Hq, Hkv, max_ctx):
+        return int(library().pq_attn_paged_workspace_bytes(int(B), int(M), int(Hq), int(Hkv), int(max_ctx)))
 
     @staticmethod
     def attn_hybrid_workspace_bytes(B, Hq, Hkv, max_ctx, win_cap):

@@ -47,6 +47,7 @@
 #include <utility>
 
 #include "pq_common.h"
+#include "pq_paged.h"
 #include "pq_polar.h"
 
 namespace {
@@ -106,6 +107,7 @@ struct AttnArgs {
     float *ws_ml; /* [piece][M * G pairs][2] */
     float *ws_o;  /* [piece][M * G pairs][128] */
     const PqDeviceConsts *consts;
+    PagedTable table; /* paged caches: where a sequence's tiles are (seq_start is not looked at) */
 };
 
 /* Work plan of one attention call, built on the device from ctx_len by the launch that
@@ -367,6 +369,13 @@ __device__ __forceinline__ int effective_ctx(const int64_t *seq_start, const int
                                              int64_t max_ctx, int64_t pool_tiles)
 {
     return effective_ctx_of(ctx_len[b], seq_start[b], max_ctx, pool_tiles); /* two independent loads */
+}
+
+/* The same of a paged sequence, whose tiles lie anywhere: only the length counts. */
+__device__ __forceinline__ int paged_ctx(const int32_t *ctx_len, int b, int64_t max_ctx)
+{
+    const int64_t c = ctx_len[b];
+    return c <= 0 ? 0 : (int)(c > max_ctx ? max_ctx : c);
 }
 
 /* Issue priority of the wavefront among those of its SIMD (0..3, scalar argument). */
@@ -660,7 +669,7 @@ __device__ __forceinline__ float wave_max_f(float x)
  * wide; at depth 7 108 and 81.  Five to eight pairs: wide_tiles.  Key tiles that went to LDS ahead of
  * their use made four pairs slower (35.1 -> 36.7 us for 32 short sequences, 112.6 -> 114.9 at 65536 tiles: the LDS is as busy as the vector
  * ALU there). */
-template <int NG, int WAVES_PER_SIMD, bool DEEP, int COPIES>
+template <int NG, int WAVES_PER_SIMD, bool DEEP, int COPIES, bool PAGED>
 __global__ __launch_bounds__(WAVES_PER_SIMD * 4 * 64, 1) void pq_attn_partial_kernel(AttnArgs a)
 {
     constexpr int kWavesPerBlock = 4 * WAVES_PER_SIMD, kThreads = kWavesPerBlock * 64;
@@ -706,7 +715,7 @@ __global__ __launch_bounds__(WAVES_PER_SIMD * 4 * 64, 1) void pq_attn_partial_ke
         st_pre = a.plan[kPlanHeader + min(bb, a.B)];
         st_last = a.plan[kPlanHeader + a.B];
         st_len = a.ctx_len[min(bb, a.B - 1)];
-        st_start = a.seq_start[min(bb, a.B - 1)];
+        if (!PAGED) st_start = a.seq_start[min(bb, a.B - 1)];
     }
     {   /* tables: the image in global memory is compact (PQ_TAB_*); the small ones are spread over a column per lane.
            All of a thread's entries are requested before the first one is stored: one trip to memory, not one per
@@ -783,8 +792,12 @@ __global__ __launch_bounds__(WAVES_PER_SIMD * 4 * 64, 1) void pq_attn_partial_ke
         const int bb = (int)threadIdx.x - kStager;
         sPre[bb] = st_pre;
         if (bb == 63) sPre[64] = st_last;
-        sCtx[bb] = bb < a.B ? effective_ctx_of(st_len, st_start, a.max_ctx, a.pool_tiles) : 0;
-        sTile0[bb] = st_start >> 6;
+        if (PAGED) {
+            sCtx[bb] = bb < a.B ? max(0, (int)min((int64_t)st_len, a.max_ctx)) : 0;
+        } else {
+            sCtx[bb] = bb < a.B ? effective_ctx_of(st_len, st_start, a.max_ctx, a.pool_tiles) : 0;
+            sTile0[bb] = st_start >> 6;
+        }
     }
     __syncthreads();
 
@@ -810,8 +823,9 @@ __global__ __launch_bounds__(WAVES_PER_SIMD * 4 * 64, 1) void pq_attn_partial_ke
         return staged ? __builtin_amdgcn_readfirstlane(sPre[i]) : a.plan[kPlanHeader + i];
     };
     auto ctx_of = [&](int bb) -> int {
-        return staged ? __builtin_amdgcn_readfirstlane(sCtx[bb])
-                      : effective_ctx(a.seq_start, a.ctx_len, bb, a.max_ctx, a.pool_tiles);
+        if (staged) return __builtin_amdgcn_readfirstlane(sCtx[bb]);
+        if constexpr (PAGED) return __builtin_amdgcn_readfirstlane(paged_ctx(a.ctx_len, bb, a.max_ctx));
+        else return effective_ctx(a.seq_start, a.ctx_len, bb, a.max_ctx, a.pool_tiles);
     };
     auto tile0_of = [&](int bb) -> int64_t {
         if (!staged) return a.seq_start[bb] >> 6;
@@ -867,14 +881,44 @@ __global__ __launch_bounds__(WAVES_PER_SIMD * 4 * 64, 1) void pq_attn_partial_ke
         if (piece_tiles <= 0) return; /* cannot happen with a consistent plan */
         const int64_t piece = (int64_t)w + (int64_t)b * a.Hkv + hk;
 
-        const int64_t seq_tile0 = tile0_of(b);
-        const int64_t stream_tile0 = (int64_t)hk * a.pool_tiles + seq_tile0;
-        /* descriptors of this sequence's tiles in the four planes (the context is at most 2^31 tokens: 32-bit sizes) */
-        const uint32_t code_bytes = (uint32_t)n_tiles * PQL_CODE_BYTES, radii_bytes = (uint32_t)n_tiles * (kRadiiHalves * 2u);
-        const __amdgpu_buffer_rsrc_t kc = stream_descriptor(a.k_codes + stream_tile0 * PQL_CODE_BYTES, code_bytes);
-        const __amdgpu_buffer_rsrc_t vc = stream_descriptor(a.v_codes + stream_tile0 * PQL_CODE_BYTES, code_bytes);
-        const __amdgpu_buffer_rsrc_t kr = stream_descriptor(a.k_radii + stream_tile0 * kRadiiHalves, radii_bytes);
-        const __amdgpu_buffer_rsrc_t vr = stream_descriptor(a.v_radii + stream_tile0 * kRadiiHalves, radii_bytes);
+        /* Descriptors of this sequence's tiles in the four planes (the context is at most 2^31 tokens: 32-bit sizes).  Paged: of the one
+           tile that was requested last, its page out of a register that holds the table's entries of 64 tiles, one per lane. */
+        __amdgpu_buffer_rsrc_t kc, vc, kr, vr;
+        int page_base = tile_lo;
+        int32_t page_reg = -1;
+        bool missing = false; /* the tile requested last has no page */
+        auto fetch_pages = [&](int t) {
+            page_base = t;
+            const int64_t i = (int64_t)b * a.table.ld_pages + min(t + lane, n_tiles - 1);
+            page_reg = a.table.pages[i];
+        };
+        auto page_of = [&](int t) -> int64_t {
+            const int p = __builtin_amdgcn_readlane(page_reg, t - page_base);
+            return p >= 0 && p < a.pool_tiles ? p : -1;
+        };
+        auto describe = [&](int64_t tile0, int n) {
+            const uint32_t code_bytes = (uint32_t)n * PQL_CODE_BYTES, radii_bytes = (uint32_t)n * (kRadiiHalves * 2u);
+            const int64_t at = (int64_t)hk * a.pool_tiles + tile0;
+            kc = stream_descriptor(a.k_codes + at * PQL_CODE_BYTES, code_bytes);
+            vc = stream_descriptor(a.v_codes + at * PQL_CODE_BYTES, code_bytes);
+            kr = stream_descriptor(a.k_radii + at * kRadiiHalves, radii_bytes);
+            vr = stream_descriptor(a.v_radii + at * kRadiiHalves, radii_bytes);
+        };
+        if constexpr (PAGED) fetch_pages(tile_lo);
+        else describe(tile0_of(b), n_tiles);
+        /* the number by which tile t is requested from the descriptors: paged, they are set to it first (a tile without a page is
+           requested from the first one of the pool; nobody looks at it) */
+        auto place = [&](int t) -> uint32_t {
+            if constexpr (PAGED) {
+                if (t - page_base >= 64) fetch_pages(t);
+                const int64_t p = page_of(t);
+                missing = p < 0;
+                describe(missing ? 0 : p, 1);
+                return 0;
+            } else {
+                return (uint32_t)t;
+            }
+        };
 
         /* ---- q' operands (see QueryOperand, WideQuery); pair p = (query token p / G, head p % G) ---- */
         std::conditional_t<WIDE, WideQuery, QueryOperand<WIDE ? 1 : NG>> qo;
@@ -919,6 +963,13 @@ __global__ __launch_bounds__(WAVES_PER_SIMD * 4 * 64, 1) void pq_attn_partial_ke
         for (int h = 0; h < kLanePairs; ++h) { m_ref[h] = 0.f; l_run[h] = 0.f; }
         bool have_ref = false; /* m_ref is a place holder until the first tile of the piece has set it */
 
+        /* wide: tile `next`'s keys on their way to LDS (behind the last tile: that one again, or none) */
+        auto request_keys = [&](int next) {
+            if (kInFlight || next < tile_hi) {
+                const uint32_t at = place(min(next, tile_hi - 1)); /* ahead of the descriptors' use */
+                request_k_tile<DEEP>(sK[wave], kc, kr, at, lane);
+            }
+        };
         /* One tile.  MASKED: the tile holds tokens beyond the context, or beyond what one of the query
          * tokens may see (lim[h]: tokens of this tile that the pair sees; nv: tokens inside the context). */
         auto do_tile = [&](auto masked_c, const KTileRaw &kraw, const VTileRaw &vraw, const int (&lim)[kLanePairs], int nv,
@@ -994,7 +1045,7 @@ __global__ __launch_bounds__(WAVES_PER_SIMD * 4 * 64, 1) void pq_attn_partial_ke
                 if (DEEP) stage_deep_value_radii(tab + T::kTUp, dr, vraw.top, lane);
                 /* the next tile's keys, once every read of this one's has returned */
                 asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-                if (kInFlight || next < tile_hi) request_k_tile<DEEP>(sK[wave], kc, kr, min(next, tile_hi - 1), lane);
+                request_keys(next);
                 if (MASKED) {
 #pragma unroll
                     for (int i = 0; i < 4; ++i)
@@ -1069,19 +1120,34 @@ __global__ __launch_bounds__(WAVES_PER_SIMD * 4 * 64, 1) void pq_attn_partial_ke
         VTileRaw vraw;
         auto request_values = [&](int t) {
             if (WIDE) asm volatile("" ::: "memory"); /* behind the keys' requests: keys_arrived */
-            load_v_tile<DEEP>(vraw, vc, vr, t, lane);
+            load_v_tile<DEEP>(vraw, vc, vr, PAGED ? 0u : (uint32_t)t, lane); /* paged: place(t) has been called */
         };
         auto request_next = [&](int t) {
             if (kInFlight) {
                 request_values(min(t, tile_hi - 1));
             } else if (t < tile_hi) {
-                if (!WIDE) load_k_tile<DEEP>(kraw, kc, kr, t, lane);
+                if (!WIDE) {
+                    const uint32_t at = place(t);
+                    load_k_tile<DEEP>(kraw, kc, kr, at, lane);
+                }
                 request_values(t);
             }
         };
-        if (WIDE) request_k_tile<DEEP>(sK[wave], kc, kr, tile_lo, lane);
-        else load_k_tile<DEEP>(kraw, kc, kr, tile_lo, lane);
+        const uint32_t at_lo = place(tile_lo);
+        if (WIDE) request_k_tile<DEEP>(sK[wave], kc, kr, at_lo, lane);
+        else load_k_tile<DEEP>(kraw, kc, kr, at_lo, lane);
         request_values(tile_lo);
+        /* paged: the tile has no page, its tokens take no part: on to the next one */
+        auto passed_over = [&](int t) {
+            if constexpr (PAGED) {
+                if (missing) {
+                    if (WIDE) request_keys(t + 1);
+                    request_next(t + 1);
+                    return true;
+                }
+            }
+            return false;
+        };
         int tile = tile_lo;
         {
             int lim[kLanePairs];
@@ -1099,11 +1165,13 @@ __global__ __launch_bounds__(WAVES_PER_SIMD * 4 * 64, 1) void pq_attn_partial_ke
                     const int ahead = (d4.x > done) + (d4.y > done) + (d4.z > done) + (d4.w > done);
                     set_wave_priority(min(__builtin_amdgcn_readfirstlane(ahead), 3));
                 }
+                if (passed_over(tile)) continue;
                 do_tile(std::false_type{}, kraw, vraw, lim, 64, tile + 1);
                 request_next(tile + 1);
             }
         }
         for (; tile < tile_hi; ++tile) { /* the masked tiles at the end of the sequence */
+            if (passed_over(tile)) continue;
             const int nv = min(ctx - tile * 64, 64);
             int lim[kLanePairs]; /* tokens of this tile that the pair may see */
 #pragma unroll
@@ -1181,6 +1249,26 @@ __global__ __launch_bounds__(WAVES_PER_SIMD * 4 * 64, 1) void pq_attn_partial_ke
     }
 }
 
+/* Groups of sequences with a common prefix: sequences start[g] .. start[g + 1] - 1 share the first length[g] tokens, max_len at most.
+ * n == 0: no prefixes. */
+struct PrefixGroups {
+    const int32_t *start, *length;
+    int n;
+    int64_t max_len;
+};
+
+__device__ __forceinline__ int group_of_sequence(const PrefixGroups &g, int b, int lane)
+{
+    const int i = paged_find(g.n, b, lane, [&](int k) { return (int64_t)g.start[k]; });
+    return i < g.n ? i : -1;
+}
+
+__device__ __forceinline__ int prefix_length(const PrefixGroups &g, int i)
+{
+    const int64_t n = g.length[i];
+    return n <= 0 ? 0 : (int)(n > g.max_len ? g.max_len : n);
+}
+
 struct RotateArgs {
     const uint16_t *q; /* bf16 [rows][128] */
     uint16_t *qrot;    /* binary16 [rows][128] */
@@ -1188,13 +1276,45 @@ struct RotateArgs {
     float scale;       /* softmax_scale * log2(e) */
     const PqDeviceConsts *consts;
     PqHadamard had;    /* on: q' = q S by a fast Walsh-Hadamard transform, S is not read */
+    RotaryArgs rot;    /* paged caches (ROT): q is rotated to its token's position first */
+    const int32_t *positions, *ctx_len; /* positions[b * M + m], or NULL: ctx_len[b] - M + m and the prefix that comes before */
+    PrefixGroups groups;
+    int M, Hq;
 };
+
+/* Position of query row `row` = (b M + m) Hq + head; the same in all lanes. */
+__device__ __forceinline__ int64_t query_position(const RotateArgs &a, int row, int lane)
+{
+    const int bm = row / a.Hq, b = bm / a.M;
+    if (a.positions) return a.positions[bm];
+    int64_t p = (int64_t)a.ctx_len[b] - a.M + (bm - b * a.M);
+    if (a.groups.n) {
+        const int g = group_of_sequence(a.groups, b, lane);
+        if (g >= 0) p += prefix_length(a.groups, g);
+    }
+    return p;
+}
+
+/* Coordinate j of query row `row`, rotated */
+template <bool ROT>
+__device__ __forceinline__ float query_element(const RotateArgs &a, int row, int j, const float *cs)
+{
+    const uint16_t *q = a.q + (int64_t)row * PQ_D;
+    float x = __uint_as_float((uint32_t)q[j] << 16);
+    if (ROT && j < a.rot.dim) {
+        const RotaryPair p = rotary_pair(a.rot, j);
+        const float s = cs[(a.rot.dim >> 1) + p.at] * __uint_as_float((uint32_t)q[p.partner] << 16);
+        x = __builtin_fmaf(x, cs[p.at], p.minus ? -s : s);
+    }
+    return x;
+}
 
 /* Four query rows per workgroup: the workgroup's slice of S (64 KB, what bounds this launch) is
  * fetched once for the four.  Thread (kq, j) accumulates the quarter kq of the sum over i for
  * column j of each row; thread (r, j) then adds the four quarters of row r in a fixed order. */
 constexpr int kRotateRows = 4;
 
+template <bool ROT = false>
 __device__ __forceinline__ void rotate_query_rows(const RotateArgs &a, int row0, int n_rows)
 {
     __shared__ float sq[kRotateRows][PQ_D];
@@ -1203,9 +1323,9 @@ __device__ __forceinline__ void rotate_query_rows(const RotateArgs &a, int row0,
     if (a.had.on) { /* S = D H / sqrt(128): wavefront w transforms row row0 + w, two elements per lane */
         const int w = tid >> 6, lane = tid & 63, hrow = row0 + w;
         if (w < kRotateRows && hrow < n_rows) {
-            const uint16_t *qr = a.q + (int64_t)hrow * PQ_D;
-            float lo = __uint_as_float((uint32_t)qr[lane] << 16) * pq_hadamard_sign(a.had, lane);
-            float hi = __uint_as_float((uint32_t)qr[lane + 64] << 16) * pq_hadamard_sign(a.had, lane + 64);
+            const float *cs = ROT ? rotary_row(a.rot, query_position(a, hrow, lane)) : nullptr;
+            float lo = query_element<ROT>(a, hrow, lane, cs) * pq_hadamard_sign(a.had, lane);
+            float hi = query_element<ROT>(a, hrow, lane + 64, cs) * pq_hadamard_sign(a.had, lane + 64);
             pq_fwht128(lo, hi, lane);
             const float c = a.scale * PQ_INV_SQRT_D;
             a.qrot[(int64_t)hrow * PQ_D + lane] = __builtin_bit_cast(uint16_t, (_Float16)(lo * c));
@@ -1216,7 +1336,13 @@ __device__ __forceinline__ void rotate_query_rows(const RotateArgs &a, int row0,
     MatrixSlice ms;
     matrix_slice_load(ms, a.S, tid);
     const int row = row0 + r;
-    sq[r][j] = row < n_rows ? __uint_as_float((uint32_t)a.q[(int64_t)row * PQ_D + j] << 16) : 0.f;
+    if constexpr (ROT) {
+        const int safe = __builtin_amdgcn_readfirstlane(min(row, n_rows - 1)); /* two wavefronts per row */
+        const float x = query_element<true>(a, safe, j, rotary_row(a.rot, query_position(a, safe, tid & 63)));
+        sq[r][j] = row < n_rows ? x : 0.f;
+    } else {
+        sq[r][j] = row < n_rows ? query_element<false>(a, row, j, nullptr) : 0.f;
+    }
     __syncthreads();
     {
         const int kq = r; /* the same thread index split serves as (quarter, column) here */
@@ -1259,7 +1385,9 @@ __device__ __forceinline__ void build_plan(const PlanArgs &a)
     int carry = 0;
     for (int base = 0; base < a.B; base += 512) {
         const int b = base + tid;
-        int v = b < a.B ? (effective_ctx(a.seq_start, a.ctx_len, b, a.max_ctx, a.pool_tiles) + 63) >> 6 : 0;
+        int v = 0;
+        if (b < a.B) /* paged caches have no seq_start */
+            v = ((a.seq_start ? effective_ctx(a.seq_start, a.ctx_len, b, a.max_ctx, a.pool_tiles) : paged_ctx(a.ctx_len, b, a.max_ctx)) + 63) >> 6;
 #pragma unroll
         for (int d = 1; d < 64; d <<= 1) {
             const int up = __shfl_up(v, d);
@@ -1305,9 +1433,10 @@ __device__ __forceinline__ void build_plan(const PlanArgs &a)
 }
 
 /* workgroups [0, row_blocks) rotate kRotateRows query rows each, the last workgroup builds the work plan */
+template <bool ROT>
 __global__ __launch_bounds__(512) void pq_rotate_q_kernel(RotateArgs a, PlanArgs p, int rows, int row_blocks)
 {
-    if ((int)blockIdx.x < row_blocks) rotate_query_rows(a, kRotateRows * (int)blockIdx.x, rows);
+    if ((int)blockIdx.x < row_blocks) rotate_query_rows<ROT>(a, kRotateRows * (int)blockIdx.x, rows);
     else build_plan(p);
 }
 
@@ -1765,6 +1894,14 @@ struct StepAppend {
     int n_heads;
 };
 
+/* a paged cache: its tables instead of seq_start, and the position rotation of the queries (optional) */
+struct StepPaged {
+    const int32_t *pages;
+    int64_t ld_pages;
+    const pq_rotary *rotary;
+    const int32_t *positions;
+};
+
 /* the unquantised recent window of hybrid attention (optional) */
 struct StepWindow {
     const void *win_k, *win_v;
@@ -1779,7 +1916,7 @@ struct StepWindow {
    the tiles of the largest context for all, as many as twice those of a mixed batch: the lines lie a little beyond the crossings at 14 and 11. */
 template <bool DEEP> constexpr int wide_tiles() { return DEEP ? 14 : 18; }
 
-template <bool DEEP>
+template <bool DEEP, bool PAGED>
 void launch_partial_depth(int pairs, int slots, dim3 grid, hipStream_t s, const AttnArgs &aa)
 {
     auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3((unsigned)(4 * waves_per_simd(pairs) * 64)), 0, s, aa); };
@@ -1787,11 +1924,11 @@ void launch_partial_depth(int pairs, int slots, dim3 grid, hipStream_t s, const 
     /* Up to two tiles per wavefront of the largest context the shorter start counts more than the gathers (copies of the quarter table, four
        against eight, us: one sequence of 1000 tokens 14.8 / 15.0, of 100 14.4 / 14.6; 32 of 200 to 4096, four tiles at most, 35.0 / 34.9).  The
        lengths are on the device: short sequences under a large largest context take eight. */
-    if (pairs <= 4 && most_tiles <= 2 * (int64_t)slots) launch(pq_attn_partial_kernel<1, 4, DEEP, 4>);
-    else if (pairs <= 4) launch(pq_attn_partial_kernel<1, 4, DEEP, 8>);
-    else if (pairs > 8) launch(pq_attn_partial_kernel<0, 2, DEEP, 1>);
-    else if (most_tiles <= (int64_t)wide_tiles<DEEP>() * slots) launch(pq_attn_partial_kernel<0, 3, DEEP, 1>);
-    else launch(pq_attn_partial_kernel<2, 3, DEEP, 8>);
+    if (pairs <= 4 && most_tiles <= 2 * (int64_t)slots) launch(pq_attn_partial_kernel<1, 4, DEEP, 4, PAGED>);
+    else if (pairs <= 4) launch(pq_attn_partial_kernel<1, 4, DEEP, 8, PAGED>);
+    else if (pairs > 8) launch(pq_attn_partial_kernel<0, 2, DEEP, 1, PAGED>);
+    else if (most_tiles <= (int64_t)wide_tiles<DEEP>() * slots) launch(pq_attn_partial_kernel<0, 3, DEEP, 1, PAGED>);
+    else launch(pq_attn_partial_kernel<2, 3, DEEP, 8, PAGED>);
 }
 
 template <int ROWS>
@@ -1812,17 +1949,22 @@ void launch_combine(int rows, bool hybrid, hipStream_t s, const CombineArgs &ca)
     else launch_combine_rows<4>(rows, hybrid, s, ca);
 }
 
-pq_status attention_launches(const pq_ctx *ctx, const StepAppend *app, const StepWindow *win, int M, const void *q,
+pq_status attention_launches(const pq_ctx *ctx, const StepAppend *app, const StepWindow *win, const StepPaged *paged, int M, const void *q,
                              void *out, pq_dtype out_dtype,
                              uint8_t *k_codes, uint16_t *k_radii, uint8_t *v_codes, uint16_t *v_radii,
                              const int64_t *seq_start, const int32_t *ctx_len,
                              int B, int Hq, int Hkv, int64_t pool_tokens, int64_t max_ctx,
                              float softmax_scale, void *workspace, size_t workspace_bytes, void *hip_stream)
 {
-    if (!ctx || !q || !out || !k_codes || !k_radii || !v_codes || !v_radii || !seq_start || !ctx_len || !workspace)
+    if (!ctx || !q || !out || !k_codes || !k_radii || !v_codes || !v_radii || (!seq_start && !paged) || !ctx_len || !workspace)
         return PQ_EINVAL;
-    if (B <= 0 || Hq <= 0 || Hkv <= 0 || pool_tokens <= 0 || (pool_tokens & 63) || max_ctx < 0 || max_ctx > pool_tokens)
+    if (B <= 0 || Hq <= 0 || Hkv <= 0 || pool_tokens <= 0 || (pool_tokens & 63) || max_ctx < 0 || (!paged && max_ctx > pool_tokens))
         return PQ_EINVAL;
+    if (paged) { /* tiles of a paged sequence may be fewer in the pool than in its table (a page that several entries name) */
+        if (!paged->pages || paged->ld_pages <= 0 || paged->ld_pages < (max_ctx + 63) / 64 || pool_tokens / 64 > 0x7FFFFFFF) return PQ_EINVAL;
+        const pq_status rs = pq_check_rotary(paged->rotary);
+        if (rs != PQ_OK) return rs;
+    }
     if (Hq % Hkv) return PQ_EINVAL;
     if (max_ctx > ((int64_t)1 << 26)) return PQ_EUNSUPPORTED; /* a sequence's tiles are addressed with 32-bit byte offsets */
     /* the work plan counts the tiles of all (sequence, kv head) streams in 31 bits (288 GB of cache hold 2^25) */
@@ -1865,7 +2007,8 @@ pq_status attention_launches(const pq_ctx *ctx, const StepAppend *app, const Ste
 
     int32_t *plan = reinterpret_cast<int32_t *>(ws + p.off_plan);
     const PlanArgs pa{seq_start, ctx_len, B, Hkv, max_ctx, pool_tokens / 64, p.slots, plan};
-    RotateArgs ra{static_cast<const uint16_t *>(q), qrot, ds->S_f32, softmax_scale * kLog2e, ds->consts, ctx->hadamard};
+    RotateArgs ra{static_cast<const uint16_t *>(q), qrot, ds->S_f32, softmax_scale * kLog2e, ds->consts, ctx->hadamard,
+                  pq_rotary_args(paged ? paged->rotary : nullptr), paged ? paged->positions : nullptr, ctx_len, PrefixGroups{}, M, Hq};
     if (app) {
         AppendArgs ak{app->xk, k_codes, k_radii, pool_tokens / 64, pool_tokens, app->dst_token, Hkv, ds->S_f32, ds->consts, ctx->hadamard};
         AppendArgs av{app->xv, v_codes, v_radii, pool_tokens / 64, pool_tokens, app->dst_token, Hkv, ds->S_f32, ds->consts, ctx->hadamard};
@@ -1888,7 +2031,9 @@ pq_status attention_launches(const pq_ctx *ctx, const StepAppend *app, const Ste
         if (per_wave == 2) hipLaunchKernelGGL(pq_rotate_window_kernel<2>, grid, blk, 0, s, ra, pa, rows, row_blocks, wa, (int)wblocks);
         else hipLaunchKernelGGL(pq_rotate_window_kernel<1>, grid, blk, 0, s, ra, pa, rows, row_blocks, wa, (int)wblocks);
     } else {
-        hipLaunchKernelGGL(pq_rotate_q_kernel, dim3((unsigned)row_blocks + 1u), dim3(512), 0, s, ra, pa, rows, row_blocks);
+        auto rotate = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((unsigned)row_blocks + 1u), dim3(512), 0, s, ra, pa, rows, row_blocks); };
+        if (ra.rot.cs) rotate(pq_rotate_q_kernel<true>);
+        else rotate(pq_rotate_q_kernel<false>);
     }
     AttnArgs aa{};
     aa.qrot = qrot;
@@ -1901,10 +2046,16 @@ pq_status attention_launches(const pq_ctx *ctx, const StepAppend *app, const Ste
     aa.n_pieces = (int)p.pieces;
     aa.ws_ml = ws_ml; aa.ws_o = ws_o;
     aa.consts = ds->consts;
+    if (paged) aa.table = PagedTable{paged->pages, paged->ld_pages, pool_tokens / 64};
     aa.up_b5 = ctx->upper_bits[0]; aa.up_b6 = ctx->upper_bits[1]; aa.up_b7 = ctx->upper_bits[2];
     pq_prof_before(0, s);
-    if (ctx->depth == 7) launch_partial_depth<true>(M * G, p.slots, dim3(p.blocks), s, aa);
-    else launch_partial_depth<false>(M * G, p.slots, dim3(p.blocks), s, aa);
+    auto partial = [&](auto paged_c) {
+        constexpr bool PAGED = decltype(paged_c)::value;
+        if (ctx->depth == 7) launch_partial_depth<true, PAGED>(M * G, p.slots, dim3(p.blocks), s, aa);
+        else launch_partial_depth<false, PAGED>(M * G, p.slots, dim3(p.blocks), s, aa);
+    };
+    if (paged) partial(std::true_type{});
+    else partial(std::false_type{});
     pq_prof_after(0, s);
 
     CombineArgs ca{ws_ml, ws_o, B, Hq, Hkv, M, plan,
@@ -1927,7 +2078,7 @@ extern "C" pq_status pq_attn_decode_polar(const pq_ctx *ctx, const void *q, void
                                           void *hip_stream)
 {
     /* the caches are only read on this path */
-    return attention_launches(ctx, nullptr, nullptr, 1, q, out, out_dtype, const_cast<uint8_t *>(k_codes),
+    return attention_launches(ctx, nullptr, nullptr, nullptr, 1, q, out, out_dtype, const_cast<uint8_t *>(k_codes),
                               const_cast<uint16_t *>(k_radii), const_cast<uint8_t *>(v_codes),
                               const_cast<uint16_t *>(v_radii), seq_start, ctx_len, B, Hq, Hkv, pool_tokens, max_ctx,
                               softmax_scale, workspace, workspace_bytes, hip_stream);
@@ -1990,7 +2141,7 @@ extern "C" pq_status pq_attn_decode_polar_static(const pq_ctx *ctx, const void *
     void *ws = nullptr;
     const pq_status st = scratch_of_current_device(&ws);
     if (st != PQ_OK) return st;
-    return attention_launches(ctx, nullptr, nullptr, 1, q, out, out_dtype, const_cast<uint8_t *>(k_codes),
+    return attention_launches(ctx, nullptr, nullptr, nullptr, 1, q, out, out_dtype, const_cast<uint8_t *>(k_codes),
                               const_cast<uint16_t *>(k_radii), const_cast<uint8_t *>(v_codes),
                               const_cast<uint16_t *>(v_radii), seq_start, ctx_len, B, Hq, Hkv, pool_tokens, max_ctx,
                               softmax_scale, ws, PQ_STATIC_SCRATCH_BYTES, hip_stream);
@@ -2005,7 +2156,7 @@ extern "C" pq_status pq_decode_step_polar(const pq_ctx *ctx, const void *xk, con
                                           void *hip_stream)
 {
     const StepAppend app{xk, xv, xt, dst_token, Hkv};
-    return attention_launches(ctx, &app, nullptr, 1, q, out, out_dtype, k_codes, k_radii, v_codes, v_radii, seq_start, ctx_len,
+    return attention_launches(ctx, &app, nullptr, nullptr, 1, q, out, out_dtype, k_codes, k_radii, v_codes, v_radii, seq_start, ctx_len,
                               B, Hq, Hkv, pool_tokens, max_ctx, softmax_scale, workspace, workspace_bytes, hip_stream);
 }
 
@@ -2019,7 +2170,7 @@ extern "C" pq_status pq_attn_decode_hybrid(const pq_ctx *ctx, const void *q, voi
                                            size_t workspace_bytes, void *hip_stream)
 {
     const StepWindow win{win_k, win_v, win_len, win_cap};
-    return attention_launches(ctx, nullptr, &win, 1, q, out, out_dtype, const_cast<uint8_t *>(k_codes),
+    return attention_launches(ctx, nullptr, &win, nullptr, 1, q, out, out_dtype, const_cast<uint8_t *>(k_codes),
                               const_cast<uint16_t *>(k_radii), const_cast<uint8_t *>(v_codes),
                               const_cast<uint16_t *>(v_radii), seq_start, ctx_len, B, Hq, Hkv, pool_tokens, max_ctx,
                               softmax_scale, workspace, workspace_bytes, hip_stream);
@@ -2033,8 +2184,26 @@ extern "C" pq_status pq_attn_decode_polar_mq(const pq_ctx *ctx, const void *q, v
                                              float softmax_scale, void *workspace, size_t workspace_bytes,
                                              void *hip_stream)
 {
-    return attention_launches(ctx, nullptr, nullptr, M, q, out, out_dtype, const_cast<uint8_t *>(k_codes),
+    return attention_launches(ctx, nullptr, nullptr, nullptr, M, q, out, out_dtype, const_cast<uint8_t *>(k_codes),
                               const_cast<uint16_t *>(k_radii), const_cast<uint8_t *>(v_codes),
                               const_cast<uint16_t *>(v_radii), seq_start, ctx_len, B, Hq, Hkv, pool_tokens, max_ctx,
                               softmax_scale, workspace, workspace_bytes, hip_stream);
+}
+
+extern "C" size_t pq_attn_paged_workspace_bytes(int B, int M, int Hq, int Hkv, int64_t max_ctx)
+{
+    return pq_attn_mq_workspace_bytes(B, M, Hq, Hkv, max_ctx);
+}
+
+extern "C" pq_status pq_attn_paged(const pq_ctx *ctx, const void *q, void *out, pq_dtype out_dtype, const pq_rotary *rotary,
+                                   const int32_t *positions, const uint8_t *k_codes, const uint16_t *k_radii,
+                                   const uint8_t *v_codes, const uint16_t *v_radii, int64_t pool_tokens,
+                                   const int32_t *pages, int64_t ld_pages, const int32_t *ctx_len,
+                                   int B, int M, int Hq, int Hkv, int64_t max_ctx, float softmax_scale,
+                                   void *workspace, size_t workspace_bytes, void *hip_stream)
+{
+    const StepPaged paged{pages, ld_pages, rotary, positions};
+    return attention_launches(ctx, nullptr, nullptr, &paged, M, q, out, out_dtype, const_cast<uint8_t *>(k_codes),
+                              const_cast<uint16_t *>(k_radii), const_cast<uint8_t *>(v_codes), const_cast<uint16_t *>(v_radii),
+                              nullptr, ctx_len, B, Hq, Hkv, pool_tokens, max_ctx, softmax_scale, workspace, workspace_bytes, hip_stream);
 }

@@ -69,9 +69,19 @@ struct PqDeviceConsts {
 #define PQ_DEEP_RADII_HALVES 128
 #define PQ_DEEP_RECORD_BYTES 50
 
+/* What settles a code in 64 bits (paged append): S and the cell boundaries in double precision. */
+struct PqExact {
+    double S[PQ_D * PQ_D]; /* S[i][j] */
+    double tan1[3];        /* tan of the boundaries pi/8, pi/4, 3 pi/8 of level 1 inside a quadrant */
+    double pseudo1[15];    /* general codebooks: pseudo-angles of the inner boundaries of level 1 (PqDeviceConsts::lut1) */
+    double tan2[3][3];     /* squared tangents of the inner boundaries of levels 2, 3, 4 */
+    double up_tan2[3][7];  /* the same of levels 5, 6, 7 (depth 7) */
+};
+
 /* Per-device constant buffers of a context (created on first use). */
 struct PqDeviceState {
     bool ready = false;
+    PqExact *exact = nullptr;         /* device */
     PqDeviceConsts *consts = nullptr; /* device */
     float *S_f32 = nullptr;           /* device [128][128], S[i][j]              */
     float *St_f32 = nullptr;          /* device [128][128], St[j][i] = S[i][j]   */

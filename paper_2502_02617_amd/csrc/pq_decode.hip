@@ -14,6 +14,7 @@
 #include <type_traits>
 
 #include "pq_common.h"
+#include "pq_paged.h"
 
 namespace {
 
@@ -38,7 +39,35 @@ struct DecodeArgs {
     const float *S;      /* S[i*128 + j] */
     int paired;          /* both strides even: two neighbouring coordinates of the output can be written at once */
     int deep;            /* recursion depth 7: the radius plane holds one word per token */
+    PagedTable table;    /* paged: which tiles, of which sequences, go to which rows */
+    PagedRows rows;
 };
+
+/* A tile of a head plane and the output rows that its slots go to: slot tau to row0 + tau, as far as that is in [lo, hi). */
+struct DecodePlace {
+    int64_t tile; /* -1, paged: a page outside the pool, whose rows are zeros */
+    int64_t row0, lo, hi;
+};
+
+/* Paged: the tiles of sequence b that hold rows are numbered from row_start[b] / 64 + 2 b on -- n rows that begin anywhere in a tile lie
+ * in n / 64 + 2 tiles at most, so the ranges do not meet, and no running sum has to be built first.  Numbers without a tile have no rows. */
+__device__ __forceinline__ DecodePlace paged_rows_of_tile(const DecodeArgs &a, int64_t u, int lane)
+{
+    DecodePlace p{-1, 0, 0, 0};
+    const int32_t *ns = a.rows.row_start;
+    auto offset = [&](int i) { return (int64_t)(max(ns[i], 0) >> 6) + 2 * i; };
+    const int b = paged_find(a.rows.n_seq, u, lane, offset);
+    if (b < 0 || b >= a.rows.n_seq) return p;
+    const int64_t end = ns[b + 1], n = end - ns[b], ctx = a.rows.ctx_len[b];
+    const int64_t first = max(ctx - n, (int64_t)0);
+    const int64_t t0 = ((first >> 6) + (u - offset(b))) * 64;
+    if (n <= 0 || t0 >= ctx) return p;
+    p.tile = paged_page(a.table, b, t0);
+    p.row0 = end - ctx + t0;
+    p.lo = max(end - ctx + first, (int64_t)0);
+    p.hi = min(end, a.rows.n_rows);
+    return p;
+}
 
 /* What a lane needs of its token: the indices of blocks 4 H .. 4 H + 3 and their radii (fp32). */
 struct TokenHalf {
@@ -195,7 +224,7 @@ __device__ __forceinline__ void dq_store_pair(void *out, int64_t at, float a, fl
  * travels under the rebuild and the products of this half tile.  (Values spill one register to bf16 and three with AHEAD, keys
  * one with AHEAD; measured as they are.)  Whole tiles on eight wavefronts of 256 registers (S fetched half as often)
  * spill 100 registers; value slots are read from an image in LDS because a token's 16 slots are spread over 16 strings. */
-template <int KIND, int OT, bool UNIT, bool AHEAD>
+template <int KIND, int OT, bool UNIT, bool AHEAD, bool PAGED>
 __global__ __launch_bounds__(kDecodeThreads, 1) void pq_decode_kernel(DecodeArgs a)
 {
     constexpr int kChunks = 4 * 8 * 64; /* of eight halves: (64-coordinate group, parity), k-step, lane */
@@ -210,9 +239,13 @@ __global__ __launch_bounds__(kDecodeThreads, 1) void pq_decode_kernel(DecodeArgs
     /* consecutive half tiles go to different workgroups: a short range occupies every CU */
     const int64_t stride = (int64_t)kDecodeWaves * gridDim.x;
     const int radii_halves = a.deep ? PQ_DEEP_RADII_HALVES : PQL_RADII;
+    auto place = [&](int64_t tile_in, int lane) {
+        if constexpr (PAGED) return paged_rows_of_tile(a, tile_in, lane);
+        else return DecodePlace{a.first_tile + tile_in, (a.first_tile + tile_in) * 64 - a.token0, 0, a.n_tokens};
+    };
     auto request = [&](int64_t item, int lane) {
-        const int64_t full_tile = item >> 1, head = full_tile / a.n_tiles, tile = a.first_tile + (full_tile - head * a.n_tiles);
-        const int64_t at = head * a.pool_tiles + tile;
+        const int64_t full_tile = item >> 1, head = full_tile / a.n_tiles;
+        const int64_t at = head * a.pool_tiles + max(place(full_tile - head * a.n_tiles, lane).tile, (int64_t)0);
         dq_request_tile(img[wave], a.codes + at * PQL_CODE_BYTES, a.radii + at * radii_halves, 2 * radii_halves, lane);
     };
     int64_t item = (int64_t)wave * gridDim.x + blockIdx.x;
@@ -267,10 +300,13 @@ __global__ __launch_bounds__(kDecodeThreads, 1) void pq_decode_kernel(DecodeArgs
 
     for (; item < a.n_items; item += stride) {
         const int lane = dq_lane(), j = lane & 31, H = lane >> 5;
-        const int64_t full_tile = item >> 1, head = full_tile / a.n_tiles, tile = a.first_tile + (full_tile - head * a.n_tiles);
+        const int64_t full_tile = item >> 1, head = full_tile / a.n_tiles;
+        const DecodePlace at_tile = place(full_tile - head * a.n_tiles, lane);
+        const int64_t tile = PAGED ? max(at_tile.tile, (int64_t)0) : at_tile.tile;
         const int half = (int)(item & 1), tau = 32 * half + j;
-        const int64_t row0 = tile * 64 + 32 * half - a.token0; /* output row of the half tile's first slot */
-        if (!AHEAD && (row0 + 32 <= 0 || row0 >= a.n_tokens)) {
+        const int64_t row0 = at_tile.row0 + 32 * half; /* output row of the half tile's first slot */
+        const int64_t row_lo = at_tile.lo, row_hi = at_tile.hi;
+        if (!AHEAD && (row0 + 32 <= row_lo || row0 >= row_hi)) {
             if (requested) asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); /* nothing writes to LDS behind the wavefront's back */
             requested = false;
             continue;
@@ -303,7 +339,12 @@ __global__ __launch_bounds__(kDecodeThreads, 1) void pq_decode_kernel(DecodeArgs
         if constexpr (AHEAD) {
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); /* and has been read: the next one may follow */
             if (item + stride < a.n_items) request(item + stride, lane);
-            if (row0 + 32 <= 0 || row0 >= a.n_tokens) continue;
+            if (row0 + 32 <= row_lo || row0 >= row_hi) continue;
+        }
+        if (PAGED && at_tile.tile < 0) { /* no page: zeros */
+#pragma unroll
+            for (int b = 0; b < 4; ++b) t.r[b] = 0.f;
+            t.top = 0;
         }
         /* the token's largest radius goes to [2^14, 2^15) */
         const uint32_t exponent = max(t.top >> 10, 1u);
@@ -337,7 +378,7 @@ __global__ __launch_bounds__(kDecodeThreads, 1) void pq_decode_kernel(DecodeArgs
         }
         dq_own_order(); /* the image is read before the next one replaces it; the scales are written */
         {
-            const bool whole = a.paired && row0 >= 0 && row0 + 32 <= a.n_tokens; /* every store of the half tile is a pair */
+            const bool whole = a.paired && row0 >= row_lo && row0 + 32 <= row_hi; /* every store of the half tile is a pair */
             /* element offset of this lane's first token, column pair 0; the rows of a register differ by scalar multiples */
             __builtin_amdgcn_sched_barrier(0);
             const int lane = dq_lane(), j = lane & 31, H = lane >> 5;
@@ -374,7 +415,7 @@ __global__ __launch_bounds__(kDecodeThreads, 1) void pq_decode_kernel(DecodeArgs
 #pragma unroll
                         for (int e = 0; e < 4; ++e) {
                             const int64_t row = row_h + 8 * r4 + e;
-                            if (WHOLE || (row >= 0 && row < a.n_tokens))
+                            if (WHOLE || (row >= row_lo && row < row_hi))
                                 dq_store_pair<OT>(a.out, at0 + (8 * r4 + e) * a.ld_token, acc[0][4 * r4 + e] * un[e],
                                                   acc[1][4 * r4 + e] * un[e], WHOLE || a.paired != 0);
                         }
@@ -456,9 +497,18 @@ void launch_decode(const DecodeArgs &a, bool unit, int rotated, int n_heads, hip
        LDS pass costs; 3001 fp32 keys 11.1 / 10.6). */
     const bool ahead = OT == PQ_F32 && a.n_items > 256 * kDecodeWaves;
     if constexpr (OT == PQ_F32)
-        if (ahead) return unit ? launch(pq_decode_kernel<KIND, OT, true, true>) : launch(pq_decode_kernel<KIND, OT, false, true>);
-    if (unit) launch(pq_decode_kernel<KIND, OT, true, false>);
-    else launch(pq_decode_kernel<KIND, OT, false, false>);
+        if (ahead) return unit ? launch(pq_decode_kernel<KIND, OT, true, true, false>) : launch(pq_decode_kernel<KIND, OT, false, true, false>);
+    if (unit) launch(pq_decode_kernel<KIND, OT, true, false, false>);
+    else launch(pq_decode_kernel<KIND, OT, false, false, false>);
+}
+
+template <int KIND, int OT>
+void launch_decode_paged(const DecodeArgs &a, bool unit, hipStream_t s)
+{
+    const dim3 grid((unsigned)(a.n_items < 256 ? a.n_items : 256));
+    auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(kDecodeThreads), 0, s, a); };
+    if (unit) launch(pq_decode_kernel<KIND, OT, true, false, true>);
+    else launch(pq_decode_kernel<KIND, OT, false, false, true>);
 }
 
 struct ExportArgs {
@@ -573,6 +623,49 @@ extern "C" pq_status pq_export_canonical(const pq_ctx *ctx, pq_kind kind, const 
     hipStream_t s = static_cast<hipStream_t>(hip_stream);
     if (kind == PQ_KEY) hipLaunchKernelGGL((pq_export_kernel<PQ_KEY>), grid, block, 0, s, a);
     else hipLaunchKernelGGL((pq_export_kernel<PQ_VALUE>), grid, block, 0, s, a);
+    PQ_HIP_TRY(hipGetLastError());
+    return PQ_OK;
+}
+
+extern "C" pq_status pq_decode_paged(const pq_ctx *ctx, const uint8_t *k_codes, const uint16_t *k_radii, const uint8_t *v_codes,
+                                     const uint16_t *v_radii, int64_t pool_tokens, const int32_t *pages, int64_t ld_pages,
+                                     const int32_t *row_start, const int32_t *ctx_len, int n_seq, int64_t n_rows, int n_heads,
+                                     void *out_k, void *out_v, pq_dtype ot, int64_t ld_token, int64_t ld_head, void *hip_stream)
+{
+    if (!ctx) return PQ_EINVAL;
+    if (n_rows == 0 || n_seq == 0) return PQ_OK;
+    if (!k_codes || !k_radii || !v_codes || !v_radii || !pages || !row_start || !ctx_len || (!out_k && !out_v)) return PQ_EINVAL;
+    if (ot != PQ_F32 && ot != PQ_BF16) return PQ_EINVAL;
+    if (n_rows < 0 || n_seq < 0 || n_heads <= 0 || pool_tokens <= 0 || (pool_tokens & 63) || ld_pages <= 0) return PQ_EINVAL;
+    if (ld_token < 0 || ld_head < 0) return PQ_EINVAL;
+    if (n_rows > 0x7FFFFFFF || pool_tokens / 64 > 0x7FFFFFFF) return PQ_EUNSUPPORTED;
+    if (!pq_aligned16(k_codes) || !pq_aligned16(k_radii) || !pq_aligned16(v_codes) || !pq_aligned16(v_radii) ||
+        (out_k && !pq_aligned16(out_k)) || (out_v && !pq_aligned16(out_v)))
+        return PQ_EALIGN;
+    const PqDeviceState *ds = nullptr;
+    const pq_status st = pq_device_state(ctx, &ds);
+    if (st != PQ_OK) return st;
+    DecodeArgs a{};
+    a.pool_tiles = pool_tokens / 64;
+    a.n_tiles = n_rows / 64 + 2 * (int64_t)n_seq;
+    a.n_items = 2 * a.n_tiles * n_heads;
+    a.ld_token = ld_token; a.ld_head = ld_head;
+    a.consts = ds->consts; a.S = ds->S_f32;
+    a.paired = ld_token % 2 == 0 && ld_head % 2 == 0;
+    a.deep = ctx->depth == 7 ? 1 : 0;
+    a.table = PagedTable{pages, ld_pages, pool_tokens / 64};
+    a.rows = PagedRows{row_start, ctx_len, n_seq, n_rows};
+    hipStream_t s = static_cast<hipStream_t>(hip_stream);
+    if (out_k) {
+        a.codes = k_codes; a.radii = k_radii; a.out = out_k;
+        if (ot == PQ_F32) launch_decode_paged<PQ_KEY, PQ_F32>(a, ctx->unit_entries, s);
+        else launch_decode_paged<PQ_KEY, PQ_BF16>(a, ctx->unit_entries, s);
+    }
+    if (out_v) {
+        a.codes = v_codes; a.radii = v_radii; a.out = out_v;
+        if (ot == PQ_F32) launch_decode_paged<PQ_VALUE, PQ_F32>(a, ctx->unit_entries, s);
+        else launch_decode_paged<PQ_VALUE, PQ_BF16>(a, ctx->unit_entries, s);
+    }
     PQ_HIP_TRY(hipGetLastError());
     return PQ_OK;
 }

@@ -314,6 +314,28 @@ void build_tables(pq_ctx *ctx)
                 for (int h = 0; h < 2; ++h) c.attn_tab[PQ_TAB_UP + 16 * l + 2 * k + h] = f2u(c.up_cs[l][k][h]);
 }
 
+void build_exact(const pq_ctx *ctx, PqExact &e)
+{
+    memset(&e, 0, sizeof(e));
+    memcpy(e.S, ctx->S, sizeof(e.S));
+    e.tan1[0] = tan(kPi / 8.0);
+    e.tan1[1] = 1.0;
+    e.tan1[2] = tan(3.0 * kPi / 8.0);
+    for (int k = 0; k < 15; ++k) e.pseudo1[k] = pseudo_angle(ctx->boundaries[0][k + 1]);
+    for (int l = 0; l < 3; ++l) {
+        for (int k = 0; k < 3; ++k) {
+            const double t = tan(ctx->boundaries[l + 1][k + 1]);
+            e.tan2[l][k] = t * t;
+        }
+        if (!ctx->general_codebooks) e.tan2[l][1] = 1.0; /* pi/4 by symmetry of the density */
+        if (ctx->depth == 7)
+            for (int k = 0; k < (1 << ctx->upper_bits[l]) - 1; ++k) {
+                const double t = tan(ctx->upper_boundaries[l][k + 1]);
+                e.up_tan2[l][k] = t * t;
+            }
+    }
+}
+
 } // namespace
 
 extern "C" const char *pq_status_string(pq_status s)
@@ -552,6 +574,7 @@ extern "C" void pq_destroy(pq_ctx *ctx)
         if (!s.ready) continue;
         if (hipSetDevice(i) != hipSuccess) continue;
         (void)hipFree(s.consts);
+        (void)hipFree(s.exact);
         (void)hipFree(s.S_f32);
         (void)hipFree(s.St_f32);
         (void)hipFree(s.S_bf16x3);
@@ -601,11 +624,14 @@ pq_status pq_device_state(const pq_ctx *cctx, const PqDeviceState **out)
                         sb[PQ_SB_TERM_STRIDE + at] = t2;
                         sb[2 * (size_t)PQ_SB_TERM_STRIDE + at] = t3;
                     }
+        std::vector<PqExact> exact(1);
+        build_exact(ctx, exact[0]);
         PqDeviceState t;
         auto release = [&t]() { /* a failed set-up leaves nothing behind: the next call starts over */
-            (void)hipFree(t.consts); (void)hipFree(t.S_f32); (void)hipFree(t.St_f32); (void)hipFree(t.S_bf16x3);
+            (void)hipFree(t.consts); (void)hipFree(t.exact); (void)hipFree(t.S_f32); (void)hipFree(t.St_f32); (void)hipFree(t.S_bf16x3);
         };
         if (hipMalloc((void **)&t.consts, sizeof(PqDeviceConsts)) != hipSuccess ||
+            hipMalloc((void **)&t.exact, sizeof(PqExact)) != hipSuccess ||
             hipMalloc((void **)&t.S_f32, Sf.size() * 4) != hipSuccess ||
             hipMalloc((void **)&t.St_f32, Stf.size() * 4) != hipSuccess ||
             hipMalloc((void **)&t.S_bf16x3, sb.size() * 2) != hipSuccess) {
@@ -613,6 +639,7 @@ pq_status pq_device_state(const pq_ctx *cctx, const PqDeviceState **out)
             return PQ_ENOMEM;
         }
         if (hipMemcpy(t.consts, &ctx->host_consts, sizeof(PqDeviceConsts), hipMemcpyHostToDevice) != hipSuccess ||
+            hipMemcpy(t.exact, exact.data(), sizeof(PqExact), hipMemcpyHostToDevice) != hipSuccess ||
             hipMemcpy(t.S_f32, Sf.data(), Sf.size() * 4, hipMemcpyHostToDevice) != hipSuccess ||
             hipMemcpy(t.St_f32, Stf.data(), Stf.size() * 4, hipMemcpyHostToDevice) != hipSuccess ||
             hipMemcpy(t.S_bf16x3, sb.data(), sb.size() * 2, hipMemcpyHostToDevice) != hipSuccess) {
