@@ -483,6 +483,32 @@ pq_status pq_attn_paged(const pq_ctx *ctx, const void *q, void *out, pq_dtype ou
 
 size_t pq_attn_paged_workspace_bytes(int B, int M, int Hq, int Hkv, int64_t max_ctx);
 
+/* pq_attn_paged for groups of sequences with a common prefix (a system prompt, a document): sequences
+ * group_start[g] .. group_start[g + 1] - 1 (device, int32 [n_groups + 1], non-decreasing)
+ * attend to the prefix_len[g] tokens (device, int32 [n_groups], at most max_prefix, itself
+ * at most 2^26) in the pages prefix_pages[g * ld_prefix_pages + ..], all of their query
+ * tokens to all of them, and behind those to their own ctx_len[b] tokens in pages[b], as
+ * in pq_attn_paged; one softmax over both.  The prefix is decoded once per 128 query rows
+ * (M * Hq/Hkv per sequence) of a group and kv head instead of once per sequence.  A
+ * prefix need not end with its last page.  Sequences in no group have no prefix;
+ * n_groups == 0 is pq_attn_paged.  rotary without positions: the position of query
+ * token m is prefix_len + ctx_len[b] - M + m.  A sequence with neither prefix nor tokens
+ * gives a zero row.  64 * ld_prefix_pages must be at least max_prefix (PQ_EINVAL).
+ * workspace: pq_attn_prefix_paged_workspace_bytes, not less (PQ_ENOMEM).  Results
+ * differ from those of pq_attn_paged on the joined page tables by the rounding of keys,
+ * once to binary16 as the rotated query is. */
+pq_status pq_attn_prefix_paged(const pq_ctx *ctx, const void *q, void *out, pq_dtype out_dtype, const pq_rotary *rotary,
+                               const int32_t *positions, const uint8_t *k_codes, const uint16_t *k_radii,
+                               const uint8_t *v_codes, const uint16_t *v_radii, int64_t pool_tokens,
+                               const int32_t *pages, int64_t ld_pages, const int32_t *ctx_len,
+                               int B, int M, int Hq, int Hkv, int64_t max_ctx,
+                               const int32_t *prefix_pages, int64_t ld_prefix_pages, const int32_t *prefix_len,
+                               const int32_t *group_start, int n_groups, int64_t max_prefix, float softmax_scale,
+                               void *workspace, size_t workspace_bytes, void *hip_stream);
+
+size_t pq_attn_prefix_paged_workspace_bytes(int B, int M, int Hq, int Hkv, int64_t max_ctx, int n_groups,
+                                            int64_t max_prefix);
+
 /* ---------------------------------------------------------------------------
  * Decode attention over a quantised prefix plus an unquantised recent window
  * (Section 5.3: the keys and values streamed in during generation are kept in

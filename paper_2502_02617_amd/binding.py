@@ -121,6 +121,11 @@ def library():
                                 ctypes.c_float, vp, ctypes.c_size_t, vp]
     L.pq_attn_paged_workspace_bytes.restype = ctypes.c_size_t
     L.pq_attn_paged_workspace_bytes.argtypes = [i32, i32, i32, i32, i64]
+    L.pq_attn_prefix_paged.restype = i32
+    L.pq_attn_prefix_paged.argtypes = [vp, vp, vp, i32, vp, vp, vp, vp, vp, vp, i64, vp, i64, vp, i32, i32, i32, i32, i64, vp, i64, vp, vp, i32,
+                                       i64, ctypes.c_float, vp, ctypes.c_size_t, vp]
+    L.pq_attn_prefix_paged_workspace_bytes.restype = ctypes.c_size_t
+    L.pq_attn_prefix_paged_workspace_bytes.argtypes = [i32, i32, i32, i32, i64, i32, i64]
     L.pq_general_record_bytes.restype = ctypes.c_size_t
     L.pq_general_record_bytes.argtypes = [vp]
     L.pq_general_codebook_entries.restype = i32
@@ -589,6 +594,26 @@ class Context:
             self._query_positions(positions, B, M), k_codes.data_ptr(), k_radii.data_ptr(), v_codes.data_ptr(), v_radii.data_ptr(),
             pool_tokens, table, ld, _ints("ctx_len", ctx_len, (B,)), B, M, Hq, heads, int(max_ctx), float(softmax_scale),
             workspace.data_ptr(), int(workspace.numel() * workspace.element_size()), _stream()))
+
+    def attn_prefix_paged(self, q, out, k_codes, k_radii, v_codes, v_radii, pages, ctx_len, max_ctx, prefix_pages, prefix_len, group_start,
+                          max_prefix, softmax_scale, workspace, rotary=None, positions=None):
+        """attn_paged with common prefixes: prefix_pages int32 [groups, pages], prefix_len int32 [groups], group_start int32 [groups + 1];
+        sequences group_start[g] .. group_start[g + 1] - 1 share prefix g, ctx_len and pages are those of their own tokens."""
+        B, M, Hq = self._paged_queries(q, out)
+        heads, pool_tokens = self._paged_cache(k_codes, k_radii, v_codes, v_radii)
+        table, ld = _pages(pages, B)
+        n_groups = prefix_len.shape[0]
+        pre_table, pre_ld = _pages(prefix_pages, n_groups)
+        _check(library().pq_attn_prefix_paged(
+            self._h, q.data_ptr(), out.data_ptr(), _dtype_code(out), ctypes.byref(rotary) if rotary is not None else None,
+            self._query_positions(positions, B, M), k_codes.data_ptr(), k_radii.data_ptr(), v_codes.data_ptr(), v_radii.data_ptr(),
+            pool_tokens, table, ld, _ints("ctx_len", ctx_len, (B,)), B, M, Hq, heads, int(max_ctx), pre_table, pre_ld,
+            _ints("prefix_len", prefix_len, (n_groups,)), _ints("group_start", group_start, (n_groups + 1,)), int(n_groups), int(max_prefix),
+            float(softmax_scale), workspace.data_ptr(), int(workspace.numel() * workspace.element_size()), _stream()))
+
+    @staticmethod
+    def attn_prefix_paged_workspace_bytes(B, M, Hq, Hkv, max_ctx, n_groups, max_prefix):
+        return int(library().pq_attn_prefix_paged_workspace_bytes(int(B), int(M), int(Hq), int(Hkv), int(max_ctx), int(n_groups), int(max_prefix)))
 
     @staticmethod
     def _paged_queries(q, out):

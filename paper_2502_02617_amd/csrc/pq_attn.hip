@@ -1377,7 +1377,8 @@ struct PlanArgs {
  * counts, 512 sequences per round (a shuffle scan inside each wavefront, then the
  * wavefronts' totals), the total and the shares of the wavefronts, and from those the first
  * wavefront and the piece count of every stream. */
-__device__ __forceinline__ void build_plan(const PlanArgs &a)
+template <typename Tiles>
+__device__ __forceinline__ void build_plan(const PlanArgs &a, Tiles tiles_of)
 {
     __shared__ int wave_sum[8];
     __shared__ uint32_t s_base, s_rem;
@@ -1385,9 +1386,7 @@ __device__ __forceinline__ void build_plan(const PlanArgs &a)
     int carry = 0;
     for (int base = 0; base < a.B; base += 512) {
         const int b = base + tid;
-        int v = 0;
-        if (b < a.B) /* paged caches have no seq_start */
-            v = ((a.seq_start ? effective_ctx(a.seq_start, a.ctx_len, b, a.max_ctx, a.pool_tiles) : paged_ctx(a.ctx_len, b, a.max_ctx)) + 63) >> 6;
+        int v = b < a.B ? tiles_of(b) : 0;
 #pragma unroll
         for (int d = 1; d < 64; d <<= 1) {
             const int up = __shfl_up(v, d);
@@ -1432,12 +1431,32 @@ __device__ __forceinline__ void build_plan(const PlanArgs &a)
     }
 }
 
+/* the plan of the sequences; paged caches have no seq_start */
+__device__ __forceinline__ void build_plan(const PlanArgs &a)
+{
+    build_plan(a, [&](int b) {
+        const int n = a.seq_start ? effective_ctx(a.seq_start, a.ctx_len, b, a.max_ctx, a.pool_tiles) : paged_ctx(a.ctx_len, b, a.max_ctx);
+        return (n + 63) >> 6;
+    });
+}
+
 /* workgroups [0, row_blocks) rotate kRotateRows query rows each, the last workgroup builds the work plan */
 template <bool ROT>
 __global__ __launch_bounds__(512) void pq_rotate_q_kernel(RotateArgs a, PlanArgs p, int rows, int row_blocks)
 {
     if ((int)blockIdx.x < row_blocks) rotate_query_rows<ROT>(a, kRotateRows * (int)blockIdx.x, rows);
     else build_plan(p);
+}
+
+#include "pq_prefix.h"
+
+/* First launch of attention with prefixes: as above, and one more workgroup builds the plan of the groups' row blocks */
+template <bool ROT>
+__global__ __launch_bounds__(512) void pq_rotate_q_prefix_kernel(RotateArgs a, PlanArgs p, PlanArgs pre, int rows, int row_blocks)
+{
+    if ((int)blockIdx.x < row_blocks) rotate_query_rows<ROT>(a, kRotateRows * (int)blockIdx.x, rows);
+    else if ((int)blockIdx.x == row_blocks) build_plan(p);
+    else build_plan(pre, [&](int i) { return row_block(a.groups, i, p.B, a.M * (a.Hq / p.Hkv), kPrefixRows).tiles; });
 }
 
 /* First launch of a whole decode step: the first workgroup builds the work plan (a chain of loads and scans, the
@@ -1484,6 +1503,11 @@ struct CombineArgs {
     const float *win_ml, *win_o;
     const int32_t *win_len;
     int n_wchunks, win_cap;
+    /* common prefixes (PREFIX): partial results of row blocks, (m, l) [piece][kPrefixRows][2] and o' likewise, and their plan */
+    const float *pre_ml, *pre_o;
+    const int32_t *pre_plan;
+    int pre_blocks;
+    PrefixGroups groups;
     PqHadamard had; /* on: the un-rotation by S^T is a fast Walsh-Hadamard transform, St is not read */
 };
 
@@ -1497,7 +1521,7 @@ struct CombineArgs {
  * Bound by the latency of its chain (plan, maxima, partial results, S^T product) up to some hundred rows, by the
  * fetches of S^T beyond: 3.9 -> 4.1 us at 32 rows, 9.2 -> 6.8 at 1024, 21.8 -> 9.4 at 2048 rows of 64 ragged
  * sequences, 17.7 -> 8.4 at 2048 rows of four query tokens (one row per workgroup, all pieces in four groups -> this). */
-template <int ROWS, bool HYBRID>
+template <int ROWS, bool HYBRID, bool PREFIX>
 __global__ __launch_bounds__(512) void pq_attn_combine_kernel(CombineArgs a, int n_rows)
 {
     constexpr int CQ = 16 / ROWS;
@@ -1537,6 +1561,21 @@ __global__ __launch_bounds__(512) void pq_attn_combine_kernel(CombineArgs a, int
         wml = a.win_ml + (int64_t)row * a.n_wchunks * 2;
         wop = a.win_o + (int64_t)row * a.n_wchunks * PQ_D + col;
     }
+    /* the pieces of this row's block over the prefix of its group */
+    int used_p = 0;
+    const float *pml = nullptr, *pop = nullptr;
+    if (PREFIX) {
+        const int g = group_of_sequence(a.groups, __builtin_amdgcn_readfirstlane(b), tid & 63); /* 32 CQ threads of a row: whole wavefronts */
+        if (g >= 0) {
+            const int i = (b - max(a.groups.start[g], 0)) * pairs + pair;
+            const int64_t block = first_block(a.groups, g, pairs, kPrefixRows) + i / kPrefixRows, stream2 = block * a.Hkv + hk;
+            const int32_t *st = a.pre_plan + kPlanHeader + a.pre_blocks + 1 + 2 * stream2;
+            const int64_t slot = (st[0] + stream2) * kPrefixRows + i % kPrefixRows;
+            used_p = st[1];
+            pml = a.pre_ml + slot * 2;
+            pop = a.pre_o + slot * PQ_D + col;
+        }
+    }
     /* overall maximum first: the 32 lanes of a group read the maxima of pieces i, 32 + i, ... together */
     float m = -INFINITY;
     {
@@ -1544,6 +1583,8 @@ __global__ __launch_bounds__(512) void pq_attn_combine_kernel(CombineArgs a, int
         for (int c = lane; c < used; c += 32) m = fmaxf(m, ml[c * ml_stride]);
         if (HYBRID)
             for (int c = lane; c < used_w; c += 32) m = fmaxf(m, wml[2 * c]);
+        if (PREFIX)
+            for (int c = lane; c < used_p; c += 32) m = fmaxf(m, pml[(int64_t)c * (2 * kPrefixRows)]);
 #pragma unroll
         for (int d = 16; d >= 1; d >>= 1) m = fmaxf(m, __shfl_xor(m, d));
     }
@@ -1559,6 +1600,12 @@ __global__ __launch_bounds__(512) void pq_attn_combine_kernel(CombineArgs a, int
 #pragma unroll 4
         for (int c = cq + CQ; c < used; c += CQ)
             add(*reinterpret_cast<const float2 *>(ml + c * ml_stride), *reinterpret_cast<const float4 *>(op + c * o_stride));
+        if (PREFIX) {
+#pragma unroll 4
+            for (int c = cq; c < used_p; c += CQ)
+                add(*reinterpret_cast<const float2 *>(pml + (int64_t)c * (2 * kPrefixRows)),
+                    *reinterpret_cast<const float4 *>(pop + (int64_t)c * (PQ_D * kPrefixRows)));
+        }
     }
     if (HYBRID) {
         for (int c = cq; c < used_w; c += CQ) {
@@ -1902,6 +1949,36 @@ struct StepPaged {
     const int32_t *positions;
 };
 
+/* groups of sequences with a common prefix (optional, paged caches) */
+struct StepPrefix {
+    const int32_t *pages; /* one row of ld_pages entries per group */
+    int64_t ld_pages;
+    const int32_t *len, *group_start;
+    int n_groups;
+    int64_t max_len;
+};
+
+/* Row blocks, pieces and workspace of the prefix's part, behind `before` bytes: plan | (m, l) | o' */
+struct PrefixPlan {
+    int n_blocks, slots;
+    size_t off_plan, off_ml, off_o, total;
+};
+
+PrefixPlan make_prefix_plan(int B, int M, int Hq, int Hkv, int n_groups, int64_t max_prefix, size_t before)
+{
+    PrefixPlan p;
+    const int pairs = M * (Hq / Hkv);
+    p.n_blocks = (int)((int64_t)B * pairs / kPrefixRows) + n_groups; /* first_block of the end */
+    const int64_t tiles = max_prefix <= 0 ? 0 : (max_prefix + 63) / 64, most = (int64_t)p.n_blocks * Hkv * tiles;
+    p.slots = (int)(most < 256 ? (most < 1 ? 1 : most) : 256); /* one workgroup per CU */
+    const size_t pieces = (size_t)p.slots + (size_t)p.n_blocks * Hkv;
+    p.off_plan = (before + 255) & ~(size_t)255;
+    p.off_ml = (p.off_plan + (kPlanHeader + (size_t)p.n_blocks + 1 + 2 * (size_t)p.n_blocks * Hkv) * sizeof(int32_t) + 255) & ~(size_t)255;
+    p.off_o = (p.off_ml + pieces * kPrefixRows * 2 * sizeof(float) + 255) & ~(size_t)255;
+    p.total = p.off_o + pieces * kPrefixRows * PQ_D * sizeof(float);
+    return p;
+}
+
 /* the unquantised recent window of hybrid attention (optional) */
 struct StepWindow {
     const void *win_k, *win_v;
@@ -1935,8 +2012,9 @@ template <int ROWS>
 void launch_combine_rows(int rows, bool hybrid, hipStream_t s, const CombineArgs &ca)
 {
     const dim3 grid((unsigned)((rows + ROWS - 1) / ROWS)), blk(512);
-    if (hybrid) hipLaunchKernelGGL((pq_attn_combine_kernel<ROWS, true>), grid, blk, 0, s, ca, rows);
-    else hipLaunchKernelGGL((pq_attn_combine_kernel<ROWS, false>), grid, blk, 0, s, ca, rows);
+    if (hybrid) hipLaunchKernelGGL((pq_attn_combine_kernel<ROWS, true, false>), grid, blk, 0, s, ca, rows);
+    else if (ca.groups.n) hipLaunchKernelGGL((pq_attn_combine_kernel<ROWS, false, true>), grid, blk, 0, s, ca, rows);
+    else hipLaunchKernelGGL((pq_attn_combine_kernel<ROWS, false, false>), grid, blk, 0, s, ca, rows);
 }
 
 void launch_combine(int rows, bool hybrid, hipStream_t s, const CombineArgs &ca)
@@ -1949,7 +2027,8 @@ void launch_combine(int rows, bool hybrid, hipStream_t s, const CombineArgs &ca)
     else launch_combine_rows<4>(rows, hybrid, s, ca);
 }
 
-pq_status attention_launches(const pq_ctx *ctx, const StepAppend *app, const StepWindow *win, const StepPaged *paged, int M, const void *q,
+pq_status attention_launches(const pq_ctx *ctx, const StepAppend *app, const StepWindow *win, const StepPaged *paged, const StepPrefix *pre,
+                             int M, const void *q,
                              void *out, pq_dtype out_dtype,
                              uint8_t *k_codes, uint16_t *k_radii, uint8_t *v_codes, uint16_t *v_radii,
                              const int64_t *seq_start, const int32_t *ctx_len,
@@ -1964,6 +2043,11 @@ pq_status attention_launches(const pq_ctx *ctx, const StepAppend *app, const Ste
         if (!paged->pages || paged->ld_pages <= 0 || paged->ld_pages < (max_ctx + 63) / 64 || pool_tokens / 64 > 0x7FFFFFFF) return PQ_EINVAL;
         const pq_status rs = pq_check_rotary(paged->rotary);
         if (rs != PQ_OK) return rs;
+    }
+    if (pre) {
+        if (!pre->pages || !pre->len || !pre->group_start || pre->n_groups <= 0 || pre->max_len < 0) return PQ_EINVAL;
+        if (pre->ld_pages <= 0 || pre->ld_pages < (pre->max_len + 63) / 64) return PQ_EINVAL;
+        if (pre->max_len > ((int64_t)1 << 26) || pre->n_groups > (1 << 24)) return PQ_EUNSUPPORTED;
     }
     if (Hq % Hkv) return PQ_EINVAL;
     if (max_ctx > ((int64_t)1 << 26)) return PQ_EUNSUPPORTED; /* a sequence's tiles are addressed with 32-bit byte offsets */
@@ -1988,12 +2072,17 @@ pq_status attention_launches(const pq_ctx *ctx, const StepAppend *app, const Ste
         if (!pq_aligned16(win->win_k) || !pq_aligned16(win->win_v)) return PQ_EALIGN;
     }
     Plan p = make_plan(B, Hq, Hkv, max_ctx, win ? win->win_cap : 0, M);
-    if (workspace_bytes < p.total) /* a smaller workspace does with larger shares */
+    if (!pre && workspace_bytes < p.total) /* a smaller workspace does with larger shares */
         p = make_plan_slots(B, Hq, Hkv, max_ctx, win ? win->win_cap : 0, M, kCoarseShareTiles);
     if ((int64_t)B * Hkv * p.n_wchunks > 0x7FFFFFFF) return PQ_EINVAL;
     /* the partial kernel addresses the rotated queries and its partial results with 32-bit byte offsets */
     if ((uint64_t)B * M * Hq * (PQ_D * 2) > 0xFFFFFFFFull || p.o_bytes > 0xFFFFFFFFull) return PQ_EUNSUPPORTED;
-    if (workspace_bytes < p.total) return PQ_ENOMEM;
+    PrefixPlan pp{};
+    if (pre) { /* the same limits for the row blocks' tiles as for the sequences' */
+        pp = make_prefix_plan(B, M, Hq, Hkv, pre->n_groups, pre->max_len, p.total);
+        if (((int64_t)B * M * G / kPrefixRows + pre->n_groups) * Hkv * ((pre->max_len + 63) / 64) >= ((int64_t)1 << 31) - 4096) return PQ_EUNSUPPORTED;
+    }
+    if (workspace_bytes < (pre ? pp.total : p.total)) return PQ_ENOMEM;
     const PqDeviceState *ds = nullptr;
     pq_status st = pq_device_state(ctx, &ds);
     if (st != PQ_OK) return st;
@@ -2008,7 +2097,9 @@ pq_status attention_launches(const pq_ctx *ctx, const StepAppend *app, const Ste
     int32_t *plan = reinterpret_cast<int32_t *>(ws + p.off_plan);
     const PlanArgs pa{seq_start, ctx_len, B, Hkv, max_ctx, pool_tokens / 64, p.slots, plan};
     RotateArgs ra{static_cast<const uint16_t *>(q), qrot, ds->S_f32, softmax_scale * kLog2e, ds->consts, ctx->hadamard,
-                  pq_rotary_args(paged ? paged->rotary : nullptr), paged ? paged->positions : nullptr, ctx_len, PrefixGroups{}, M, Hq};
+                  pq_rotary_args(paged ? paged->rotary : nullptr), paged ? paged->positions : nullptr, ctx_len,
+                  pre ? PrefixGroups{pre->group_start, pre->len, pre->n_groups, pre->max_len} : PrefixGroups{}, M, Hq};
+    int32_t *pre_plan = reinterpret_cast<int32_t *>(ws + pp.off_plan);
     if (app) {
         AppendArgs ak{app->xk, k_codes, k_radii, pool_tokens / 64, pool_tokens, app->dst_token, Hkv, ds->S_f32, ds->consts, ctx->hadamard};
         AppendArgs av{app->xv, v_codes, v_radii, pool_tokens / 64, pool_tokens, app->dst_token, Hkv, ds->S_f32, ds->consts, ctx->hadamard};
@@ -2030,6 +2121,11 @@ pq_status attention_launches(const pq_ctx *ctx, const StepAppend *app, const Ste
         const dim3 grid((unsigned)(row_blocks + 1 + wblocks)), blk(512);
         if (per_wave == 2) hipLaunchKernelGGL(pq_rotate_window_kernel<2>, grid, blk, 0, s, ra, pa, rows, row_blocks, wa, (int)wblocks);
         else hipLaunchKernelGGL(pq_rotate_window_kernel<1>, grid, blk, 0, s, ra, pa, rows, row_blocks, wa, (int)wblocks);
+    } else if (pre) {
+        const PlanArgs pb{nullptr, nullptr, pp.n_blocks, Hkv, 0, 0, pp.slots, pre_plan};
+        auto rotate = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((unsigned)row_blocks + 2u), dim3(512), 0, s, ra, pa, pb, rows, row_blocks); };
+        if (ra.rot.cs) rotate(pq_rotate_q_prefix_kernel<true>);
+        else rotate(pq_rotate_q_prefix_kernel<false>);
     } else {
         auto rotate = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((unsigned)row_blocks + 1u), dim3(512), 0, s, ra, pa, rows, row_blocks); };
         if (ra.rot.cs) rotate(pq_rotate_q_kernel<true>);
@@ -2056,12 +2152,22 @@ pq_status attention_launches(const pq_ctx *ctx, const StepAppend *app, const Ste
     };
     if (paged) partial(std::true_type{});
     else partial(std::false_type{});
+    if (pre) {
+        const PrefixArgs xa{qrot, k_codes, v_codes, k_radii, v_radii, ctx->upper_bits[0], ctx->upper_bits[1], ctx->upper_bits[2],
+                            PagedTable{pre->pages, pre->ld_pages, pool_tokens / 64}, ra.groups, B, Hq, Hkv, M, pre_plan, pp.n_blocks,
+                            reinterpret_cast<float *>(ws + pp.off_ml), reinterpret_cast<float *>(ws + pp.off_o), ds->consts};
+        auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((unsigned)pp.slots), dim3(kPrefixThreads), 0, s, xa); };
+        if (ctx->depth == 7) launch(pq_attn_prefix_kernel<4, true>);
+        else launch(pq_attn_prefix_kernel<4, false>);
+    }
     pq_prof_after(0, s);
 
     CombineArgs ca{ws_ml, ws_o, B, Hq, Hkv, M, plan,
                    ds->St_f32, out, out_dtype == PQ_F32 ? 1 : 0, ds->consts,
                    reinterpret_cast<const float *>(ws + p.off_wml), reinterpret_cast<const float *>(ws + p.off_wo),
-                   win ? win->win_len : nullptr, p.n_wchunks, win ? (int)win->win_cap : 0, ctx->hadamard};
+                   win ? win->win_len : nullptr, p.n_wchunks, win ? (int)win->win_cap : 0,
+                   reinterpret_cast<const float *>(ws + pp.off_ml), reinterpret_cast<const float *>(ws + pp.off_o), pre_plan, pp.n_blocks,
+                   ra.groups, ctx->hadamard};
     launch_combine(rows, win != nullptr, s, ca);
     PQ_HIP_TRY(hipGetLastError());
     return PQ_OK;
@@ -2078,7 +2184,7 @@ extern "C" pq_status pq_attn_decode_polar(const pq_ctx *ctx, const void *q, void
                                           void *hip_stream)
 {
     /* the caches are only read on this path */
-    return attention_launches(ctx, nullptr, nullptr, nullptr, 1, q, out, out_dtype, const_cast<uint8_t *>(k_codes),
+    return attention_launches(ctx, nullptr, nullptr, nullptr, nullptr, 1, q, out, out_dtype, const_cast<uint8_t *>(k_codes),
                               const_cast<uint16_t *>(k_radii), const_cast<uint8_t *>(v_codes),
                               const_cast<uint16_t *>(v_radii), seq_start, ctx_len, B, Hq, Hkv, pool_tokens, max_ctx,
                               softmax_scale, workspace, workspace_bytes, hip_stream);
@@ -2141,7 +2247,7 @@ extern "C" pq_status pq_attn_decode_polar_static(const pq_ctx *ctx, const void *
     void *ws = nullptr;
     const pq_status st = scratch_of_current_device(&ws);
     if (st != PQ_OK) return st;
-    return attention_launches(ctx, nullptr, nullptr, nullptr, 1, q, out, out_dtype, const_cast<uint8_t *>(k_codes),
+    return attention_launches(ctx, nullptr, nullptr, nullptr, nullptr, 1, q, out, out_dtype, const_cast<uint8_t *>(k_codes),
                               const_cast<uint16_t *>(k_radii), const_cast<uint8_t *>(v_codes),
                               const_cast<uint16_t *>(v_radii), seq_start, ctx_len, B, Hq, Hkv, pool_tokens, max_ctx,
                               softmax_scale, ws, PQ_STATIC_SCRATCH_BYTES, hip_stream);
@@ -2156,7 +2262,7 @@ extern "C" pq_status pq_decode_step_polar(const pq_ctx *ctx, const void *xk, con
                                           void *hip_stream)
 {
     const StepAppend app{xk, xv, xt, dst_token, Hkv};
-    return attention_launches(ctx, &app, nullptr, nullptr, 1, q, out, out_dtype, k_codes, k_radii, v_codes, v_radii, seq_start, ctx_len,
+    return attention_launches(ctx, &app, nullptr, nullptr, nullptr, 1, q, out, out_dtype, k_codes, k_radii, v_codes, v_radii, seq_start, ctx_len,
                               B, Hq, Hkv, pool_tokens, max_ctx, softmax_scale, workspace, workspace_bytes, hip_stream);
 }
 
@@ -2170,7 +2276,7 @@ extern "C" pq_status pq_attn_decode_hybrid(const pq_ctx *ctx, const void *q, voi
                                            size_t workspace_bytes, void *hip_stream)
 {
     const StepWindow win{win_k, win_v, win_len, win_cap};
-    return attention_launches(ctx, nullptr, &win, nullptr, 1, q, out, out_dtype, const_cast<uint8_t *>(k_codes),
+    return attention_launches(ctx, nullptr, &win, nullptr, nullptr, 1, q, out, out_dtype, const_cast<uint8_t *>(k_codes),
                               const_cast<uint16_t *>(k_radii), const_cast<uint8_t *>(v_codes),
                               const_cast<uint16_t *>(v_radii), seq_start, ctx_len, B, Hq, Hkv, pool_tokens, max_ctx,
                               softmax_scale, workspace, workspace_bytes, hip_stream);
@@ -2184,7 +2290,7 @@ extern "C" pq_status pq_attn_decode_polar_mq(const pq_ctx *ctx, const void *q, v
                                              float softmax_scale, void *workspace, size_t workspace_bytes,
                                              void *hip_stream)
 {
-    return attention_launches(ctx, nullptr, nullptr, nullptr, M, q, out, out_dtype, const_cast<uint8_t *>(k_codes),
+    return attention_launches(ctx, nullptr, nullptr, nullptr, nullptr, M, q, out, out_dtype, const_cast<uint8_t *>(k_codes),
                               const_cast<uint16_t *>(k_radii), const_cast<uint8_t *>(v_codes),
                               const_cast<uint16_t *>(v_radii), seq_start, ctx_len, B, Hq, Hkv, pool_tokens, max_ctx,
                               softmax_scale, workspace, workspace_bytes, hip_stream);
@@ -2203,7 +2309,30 @@ extern "C" pq_status pq_attn_paged(const pq_ctx *ctx, const void *q, void *out, 
                                    void *workspace, size_t workspace_bytes, void *hip_stream)
 {
     const StepPaged paged{pages, ld_pages, rotary, positions};
-    return attention_launches(ctx, nullptr, nullptr, &paged, M, q, out, out_dtype, const_cast<uint8_t *>(k_codes),
+    return attention_launches(ctx, nullptr, nullptr, &paged, nullptr, M, q, out, out_dtype, const_cast<uint8_t *>(k_codes),
+                              const_cast<uint16_t *>(k_radii), const_cast<uint8_t *>(v_codes), const_cast<uint16_t *>(v_radii),
+                              nullptr, ctx_len, B, Hq, Hkv, pool_tokens, max_ctx, softmax_scale, workspace, workspace_bytes, hip_stream);
+}
+
+extern "C" size_t pq_attn_prefix_paged_workspace_bytes(int B, int M, int Hq, int Hkv, int64_t max_ctx, int n_groups, int64_t max_prefix)
+{
+    if (B <= 0 || M <= 0 || Hq <= 0 || Hkv <= 0 || Hq % Hkv || max_ctx < 0 || n_groups < 0 || max_prefix < 0) return 0;
+    const size_t own = workspace_size(B, Hq, Hkv, max_ctx, 0, M);
+    return n_groups == 0 ? own : make_prefix_plan(B, M, Hq, Hkv, n_groups, max_prefix, own).total;
+}
+
+extern "C" pq_status pq_attn_prefix_paged(const pq_ctx *ctx, const void *q, void *out, pq_dtype out_dtype, const pq_rotary *rotary,
+                                          const int32_t *positions, const uint8_t *k_codes, const uint16_t *k_radii,
+                                          const uint8_t *v_codes, const uint16_t *v_radii, int64_t pool_tokens,
+                                          const int32_t *pages, int64_t ld_pages, const int32_t *ctx_len,
+                                          int B, int M, int Hq, int Hkv, int64_t max_ctx,
+                                          const int32_t *prefix_pages, int64_t ld_prefix_pages, const int32_t *prefix_len,
+                                          const int32_t *group_start, int n_groups, int64_t max_prefix, float softmax_scale,
+                                          void *workspace, size_t workspace_bytes, void *hip_stream)
+{
+    const StepPaged paged{pages, ld_pages, rotary, positions};
+    const StepPrefix pre{prefix_pages, ld_prefix_pages, prefix_len, group_start, n_groups, max_prefix};
+    return attention_launches(ctx, nullptr, nullptr, &paged, n_groups == 0 ? nullptr : &pre, M, q, out, out_dtype, const_cast<uint8_t *>(k_codes),
                               const_cast<uint16_t *>(k_radii), const_cast<uint8_t *>(v_codes), const_cast<uint16_t *>(v_radii),
                               nullptr, ctx_len, B, Hq, Hkv, pool_tokens, max_ctx, softmax_scale, workspace, workspace_bytes, hip_stream);
 }

@@ -1,0 +1,191 @@
+"""GPU tests of attention with common prefixes (pq_attn_prefix_paged) against attention in 64 bits over prefix and own tokens.
+Tolerance: 2e-3 as for the other calls; the keys' rounding to binary16, 2^-11 of an element, is one more of the size of the query's."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2502_02617_amd import Context, Rotary
+from tests import helpers, paged_ref
+from tests.test_gpu_paged import DEV, check_rows, dev32, f64, filled, fmt, say
+
+pytestmark = pytest.mark.gpu
+
+
+class Batch:
+    """Groups of sequences; sizes: sequences of every group, prefix: its length, own: lengths of all sequences (ungrouped ones `ahead` and
+    `behind` the groups among them)."""
+
+    def __init__(self, f, seed, sizes, prefix, own, Hkv, ahead=0, missing=()):
+        self.f, self.Hkv, self.own, self.prefix = f, Hkv, own, prefix
+        self.start = list(np.cumsum([ahead] + list(sizes)))
+        self.group = [-1] * ahead + [g for g, n in enumerate(sizes) for _ in range(n)] + [-1] * (len(own) - self.start[-1])
+        rng = np.random.default_rng(seed)
+        lens = list(prefix) + list(own)
+        self.cache, pages, vectors = filled(f, rng, lens, Hkv, 2 + sum((n + 63) // 64 for n in lens))
+        n = len(prefix)
+        self.pre_pages, self.pages, self.pre_vectors, self.vectors = pages[:n].copy(), pages[n:].copy(), vectors[:n], vectors[n:]
+        self.missing = missing
+        for g, p in missing:
+            self.pre_pages[g, p] = -1 if p % 2 else self.cache.kc.shape[1]
+
+    def run(self, q, out_dtype=torch.float32, max_prefix=None, max_ctx=None, **kw):
+        B, M, Hq, _ = q.shape
+        max_prefix, max_ctx = max_prefix or max(self.prefix), max_ctx if max_ctx is not None else max(self.own)
+        out = torch.full(q.shape, float("nan"), dtype=out_dtype, device=DEV)
+        n = Context.attn_prefix_paged_workspace_bytes(B, M, Hq, self.Hkv, max_ctx, len(self.prefix), max_prefix)
+        ws = torch.full((n,), 0xFF, dtype=torch.uint8, device=DEV)
+        self.f.ctx.attn_prefix_paged(q, out, *self.cache.all, dev32(self.pages), dev32(self.own), max_ctx, dev32(self.pre_pages),
+                                     dev32(self.prefix), dev32(self.start), max_prefix, helpers.softmax_scale(), ws, **kw)
+        torch.cuda.synchronize()
+        return out
+
+    def want(self, q, table=None, interleaved=False, positions=None):
+        M, out = q.shape[1], np.zeros(q.shape)
+        for b, n in enumerate(self.own):
+            g = self.group[b]
+            P = self.prefix[g] if g >= 0 else 0
+            keep = np.ones(P, bool)
+            for h, p in self.missing:
+                if h == g:
+                    keep[64 * p : 64 * p + 64] = False
+            qb = q[b]
+            if table is not None:
+                qb = paged_ref.rotate(qb, positions[b] if positions is not None else np.arange(P + n - M, P + n), table, interleaved)
+
+            def part(kind, h):
+                before = self.pre_vectors[g][kind][h][keep] if g >= 0 else np.zeros((0, 128))
+                return lambda m: np.concatenate([before, self.vectors[b][kind][h][: max(0, n - (M - 1 - m))]])
+
+            out[b] = paged_ref.attention(qb, [part(0, h) for h in range(self.Hkv)], [part(1, h) for h in range(self.Hkv)], helpers.softmax_scale(), M)
+        return out
+
+    def total(self):
+        return [n + (self.prefix[g] if g >= 0 else 0) for n, g in zip(self.own, self.group)]
+
+
+def queries(B, M, Hq, seed):
+    return torch.randn(B, M, Hq, 128, generator=torch.Generator().manual_seed(seed)).to(torch.bfloat16).to(DEV)
+
+
+SHAPES = [  # sizes, prefix, own, Hq, Hkv, M, ahead
+    ([3], [200], [1, 70, 0], 8, 2, 1, 0),
+    ([2], [1], [5, 64], 4, 4, 1, 0),                                            # one token
+    ([1, 0, 4, 2], [130, 64, 0, 33], [3, 0, 1, 100, 65, 2, 64], 7, 1, 2, 0),     # an empty group, an empty prefix, half a tile
+    ([5, 6], [1000, 777], [0, 9, 300, 1, 1, 20, 0, 64, 128, 7, 2, 40, 50], 14, 2, 1, 1),   # sequences ahead of the groups and behind
+    ([40], [300], [(7 * i) % 90 for i in range(40)], 4, 1, 1, 0),                # rows of two blocks
+    ([9, 35], [150, 450], [(5 * i) % 70 for i in range(44)], 16, 1, 1, 0),       # 144 and 560 rows
+    ([12], [260], [3 + (5 * i) % 70 for i in range(12)], 8, 1, 2, 0),
+]
+
+
+@pytest.mark.parametrize("name", ["general", "hadamard", "books", "deep"])
+@pytest.mark.parametrize("shape", range(len(SHAPES)))
+def test_prefix_attention(name, shape):
+    sizes, prefix, own, Hq, Hkv, M, ahead = SHAPES[shape]
+    batch = Batch(fmt(name), shape, sizes, prefix, own, Hkv, ahead)
+    B = len(own)
+    say(f"attn_prefix_paged {name} {sizes} {prefix}")
+    q = queries(B, M, Hq, shape)
+    table, inter = paged_ref.cos_sin(900, 64 if shape % 2 else 128), shape % 2 == 1
+    got = batch.run(q, rotary=Rotary(torch.from_numpy(table).to(DEV), inter))
+    check_rows(f64(got), batch.want(f64(q), table, inter), batch.total())
+    plain = batch.run(q)
+    check_rows(f64(plain), batch.want(f64(q)), batch.total())
+    assert torch.equal(batch.run(q, torch.bfloat16), plain.to(torch.bfloat16))
+    assert torch.equal(batch.run(q), plain)      # equal calls give equal bits
+
+
+def test_long_prefix_in_many_pieces_with_missing_pages():
+    """4170 tokens of one kv head over all workgroups, a page missing in the middle, the first and the last tile."""
+    batch = Batch(fmt("general"), 5, [33], [64 * 65 + 10], [i for i in range(33)], 1, 0, missing=[(0, 0), (0, 30), (0, 65)])
+    q = queries(33, 1, 8, 5)
+    check_rows(f64(batch.run(q)), batch.want(f64(q)), batch.total())
+
+
+def test_a_prefix_without_any_page_and_no_tokens():
+    batch = Batch(fmt("general"), 6, [2, 2], [100, 128], [0, 0, 0, 5], 2, 0, missing=[(0, 0), (0, 1)])
+    q = queries(4, 1, 4, 6)
+    got = f64(batch.run(q, max_ctx=64))
+    assert np.all(got[:2] == 0)
+    check_rows(got, batch.want(f64(q)), [0, 0, 128, 133])
+
+
+@pytest.mark.parametrize("size", [1e-3, 30.0])
+def test_small_and_large_keys(size):
+    """Scores of a thousandth and of thirty times the usual size.  Two roundings to binary16 of rms 2e-4 in each of a score's 128 products leave 2.8e-4
+    of its rms: nothing at a thousandth, 0.85 % of the weights' exponent at 30 (scores of rms 30); 2e-2 is 2.4 times that."""
+    f = fmt("general")
+    batch = Batch(f, 7, [20], [500], [10] * 20, 1)
+    q = (queries(20, 1, 8, 7).float() * size).to(torch.bfloat16)
+    ref, got = batch.want(f64(q)), f64(batch.run(q))
+    assert helpers.rel_l2(got, ref) <= (2e-3 if size < 1 else 2e-2)
+
+
+def test_prefix_equals_joined_tables():
+    """The same tokens as one sequence: attn_paged on the joined page tables."""
+    f = fmt("general")
+    batch = Batch(f, 8, [6, 5], [320, 64], [1, 64, 100, 7, 65, 30, 2, 3, 200, 9, 128], 2)
+    q = queries(11, 1, 8, 8)
+    table = Rotary(torch.from_numpy(paged_ref.cos_sin(600, 128)).to(DEV))
+    joined = np.full((11, 12), -1)
+    for b, g in enumerate(batch.group):
+        k, own = batch.prefix[g] // 64, (batch.own[b] + 63) // 64
+        joined[b, :k] = batch.pre_pages[g, :k]
+        joined[b, k : k + own] = batch.pages[b, :own]
+    lens = batch.total()
+    out = torch.empty(q.shape, device=DEV)
+    ws = torch.empty(Context.attn_paged_workspace_bytes(11, 1, 8, 2, 500), dtype=torch.uint8, device=DEV)
+    f.ctx.attn_paged(q, out, *batch.cache.all, dev32(joined), dev32(lens), 500, helpers.softmax_scale(), ws, rotary=table)
+    torch.cuda.synchronize()
+    assert helpers.rel_l2(f64(batch.run(q, rotary=table)), f64(out)) <= 2e-3
+    positions = dev32([[n - 1] for n in lens])
+    assert torch.equal(batch.run(q, rotary=table, positions=positions), batch.run(q, rotary=table))
+
+
+def test_no_groups_is_attn_paged():
+    f = fmt("general")
+    batch = Batch(f, 9, [], [], [1, 64, 100], 2)
+    q = queries(3, 1, 8, 9)
+    out = torch.full(q.shape, float("nan"), device=DEV)
+    ws = torch.empty(Context.attn_prefix_paged_workspace_bytes(3, 1, 8, 2, 100, 0, 0), dtype=torch.uint8, device=DEV)
+    none = torch.zeros(0, 1, dtype=torch.int32, device=DEV)
+    f.ctx.attn_prefix_paged(q, out, *batch.cache.all, dev32(batch.pages), dev32(batch.own), 100, none, none[:, 0], dev32([0]), 0,
+                            helpers.softmax_scale(), ws)
+    torch.cuda.synchronize()
+    check_rows(f64(out), batch.want(f64(q)), batch.own)
+
+
+def test_captured_with_lengths_that_grow():
+    f = fmt("general")
+    batch = Batch(f, 10, [3, 4], [190, 70], [30, 60, 1, 64, 10, 20, 90], 2)
+    q, M = torch.zeros(7, 1, 8, 128, dtype=torch.bfloat16, device=DEV), 1
+    out, eager = torch.zeros(q.shape, device=DEV), torch.zeros(q.shape, device=DEV)
+    ws = torch.empty(Context.attn_prefix_paged_workspace_bytes(7, M, 8, 2, 90, 2, 190), dtype=torch.uint8, device=DEV)
+    own, prefix = dev32([0] * 7), dev32([0, 0])
+    args = dev32(batch.pages), dev32(batch.pre_pages), dev32(batch.start)
+    f.ctx.prepare_device()
+
+    def call(o):
+        f.ctx.attn_prefix_paged(q, o, *batch.cache.all, args[0], own, 90, args[1], prefix, args[2], 190, helpers.softmax_scale(), ws)
+
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call(out)
+    full_own, full_prefix = list(batch.own), list(batch.prefix)
+    for i in range(4):
+        batch.own = [max(0, n - 10 * (3 - i)) for n in full_own]
+        batch.prefix = [max(0, n - 50 * (3 - i)) for n in full_prefix]
+        own.copy_(dev32(batch.own))
+        prefix.copy_(dev32(batch.prefix))
+        q.copy_(queries(7, 1, 8, 100 + i))
+        graph.replay()
+        torch.cuda.synchronize()
+        short = Batch.__new__(Batch)
+        short.__dict__.update(batch.__dict__)
+        short.vectors = [[[x[:n] for x in kind] for kind in v] for v, n in zip(batch.vectors, batch.own)]
+        short.pre_vectors = [[[x[:n] for x in kind] for kind in v] for v, n in zip(batch.pre_vectors, batch.prefix)]
+        check_rows(f64(out), short.want(f64(q)), short.total())
+        call(eager)
+        torch.cuda.synchronize()
+        assert torch.equal(eager, out)

@@ -46,6 +46,13 @@ def attend(ctx, **kw):
     return library().pq_attn_paged(*a.values())
 
 
+def attend_prefix(ctx, **kw):
+    a = dict(handle=ctx._h, q=P, out=P, ot=PQ_F32, rot=None, positions=None, kc=P, kr=P, vc=P, vr=P, pool=640, pages=P, ld_pages=10, ctx_len=P, B=2, M=1,
+             Hq=8, Hkv=2, max_ctx=600, pre_pages=P, pre_ld=5, pre_len=P, start=P, groups=1, max_prefix=300, scale=0.1, ws=P, ws_bytes=1 << 30, stream=None)
+    a.update(kw)
+    return library().pq_attn_prefix_paged(*a.values())
+
+
 @pytest.mark.parametrize("call", [append, decode])
 @pytest.mark.parametrize("kw,code", [
     (dict(handle=None), EINVAL), (dict(kc=None), EINVAL), (dict(vr=None), EINVAL), (dict(pages=None), EINVAL), (dict(row_start=None), EINVAL),
@@ -86,6 +93,24 @@ def test_refusals_of_decode(ctx, kw, code):
     (dict(ld_pages=1 << 24, max_ctx=(1 << 26) + 1), EUNSUPPORTED)])
 def test_refusals_of_attention(ctx, kw, code):
     assert attend(ctx, **kw) == code
+
+
+@pytest.mark.parametrize("kw,code", [
+    (dict(handle=None), EINVAL), (dict(pre_pages=None), EINVAL), (dict(pre_len=None), EINVAL), (dict(start=None), EINVAL), (dict(groups=-1), EINVAL),
+    (dict(max_prefix=-1), EINVAL), (dict(pre_ld=0), EINVAL), (dict(pre_ld=4), EINVAL), (dict(groups=(1 << 24) + 1), EUNSUPPORTED),
+    (dict(pre_ld=1 << 21, max_prefix=(1 << 26) + 1), EUNSUPPORTED), (dict(pre_ld=1 << 20, max_prefix=1 << 26, groups=2000, ws_bytes=1 << 60), EUNSUPPORTED),
+    (dict(max_ctx=641), EINVAL), (dict(M=5), EUNSUPPORTED), (dict(q=P + 8), EALIGN), (dict(ws_bytes=1000), ENOMEM),
+    (dict(ws_bytes=Context.attn_prefix_paged_workspace_bytes(2, 1, 8, 2, 600, 1, 300) - 1), ENOMEM), (dict(rot=rotary(n_pos=-1)), EINVAL)])
+def test_refusals_of_attention_with_prefixes(ctx, kw, code):
+    assert attend_prefix(ctx, **kw) == code
+
+
+def test_workspace_with_prefixes():
+    own = Context.attn_paged_workspace_bytes(4, 1, 32, 8, 100)
+    assert Context.attn_prefix_paged_workspace_bytes(4, 1, 32, 8, 100, 0, 0) == own
+    sizes = [Context.attn_prefix_paged_workspace_bytes(B, 1, 32, 8, 100, 2, n) for B, n in ((4, 0), (4, 100), (4, 5000), (64, 5000))]
+    assert own < sizes[0] <= sizes[1] <= sizes[2] <= sizes[3]
+    assert Context.attn_prefix_paged_workspace_bytes(4, 1, 7, 2, 100, 1, 100) == 0
 
 
 def test_workspace_is_that_of_several_query_tokens():
