@@ -76,6 +76,11 @@ struct PqExact {
     double pseudo1[15];    /* general codebooks: pseudo-angles of the inner boundaries of level 1 (PqDeviceConsts::lut1) */
     double tan2[3][3];     /* squared tangents of the inner boundaries of levels 2, 3, 4 */
     double up_tan2[3][7];  /* the same of levels 5, 6, 7 (depth 7) */
+    /* Which codes 32 bits leave in doubt (paged append of whole tiles): weights that make the distances of a node's inputs from its
+       boundaries comparable, 1 / (sin t (1 + tan t)) of boundary t of levels 2, 3, 4 and 5, 6, 7, and the inner boundaries' pseudo-angles
+       of level 1 between 0 and 4. */
+    float doubt[3][3], up_doubt[3][7];
+    float pseudo1_f[17];
 };
 
 /* Per-device constant buffers of a context (created on first use). */

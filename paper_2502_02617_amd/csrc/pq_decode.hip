@@ -49,26 +49,6 @@ struct DecodePlace {
     int64_t row0, lo, hi;
 };
 
-/* Paged: the tiles of sequence b that hold rows are numbered from row_start[b] / 64 + 2 b on -- n rows that begin anywhere in a tile lie
- * in n / 64 + 2 tiles at most, so the ranges do not meet, and no running sum has to be built first.  Numbers without a tile have no rows. */
-__device__ __forceinline__ DecodePlace paged_rows_of_tile(const DecodeArgs &a, int64_t u, int lane)
-{
-    DecodePlace p{-1, 0, 0, 0};
-    const int32_t *ns = a.rows.row_start;
-    auto offset = [&](int i) { return (int64_t)(max(ns[i], 0) >> 6) + 2 * i; };
-    const int b = paged_find(a.rows.n_seq, u, lane, offset);
-    if (b < 0 || b >= a.rows.n_seq) return p;
-    const int64_t end = ns[b + 1], n = end - ns[b], ctx = a.rows.ctx_len[b];
-    const int64_t first = max(ctx - n, (int64_t)0);
-    const int64_t t0 = ((first >> 6) + (u - offset(b))) * 64;
-    if (n <= 0 || t0 >= ctx) return p;
-    p.tile = paged_page(a.table, b, t0);
-    p.row0 = end - ctx + t0;
-    p.lo = max(end - ctx + first, (int64_t)0);
-    p.hi = min(end, a.rows.n_rows);
-    return p;
-}
-
 /* What a lane needs of its token: the indices of blocks 4 H .. 4 H + 3 and their radii (fp32). */
 struct TokenHalf {
     uint32_t q[4][4], bi[4];
@@ -240,8 +220,10 @@ __global__ __launch_bounds__(kDecodeThreads, 1) void pq_decode_kernel(DecodeArgs
     const int64_t stride = (int64_t)kDecodeWaves * gridDim.x;
     const int radii_halves = a.deep ? PQ_DEEP_RADII_HALVES : PQL_RADII;
     auto place = [&](int64_t tile_in, int lane) {
-        if constexpr (PAGED) return paged_rows_of_tile(a, tile_in, lane);
-        else return DecodePlace{a.first_tile + tile_in, (a.first_tile + tile_in) * 64 - a.token0, 0, a.n_tokens};
+        if constexpr (PAGED) {
+            const PagedTile p = paged_tile(a.table, a.rows, tile_in, lane);
+            return DecodePlace{p.page, p.row0, p.lo, p.hi};
+        } else return DecodePlace{a.first_tile + tile_in, (a.first_tile + tile_in) * 64 - a.token0, 0, a.n_tokens};
     };
     auto request = [&](int64_t item, int lane) {
         const int64_t full_tile = item >> 1, head = full_tile / a.n_tiles;
@@ -647,7 +629,7 @@ extern "C" pq_status pq_decode_paged(const pq_ctx *ctx, const uint8_t *k_codes, 
     if (st != PQ_OK) return st;
     DecodeArgs a{};
     a.pool_tiles = pool_tokens / 64;
-    a.n_tiles = n_rows / 64 + 2 * (int64_t)n_seq;
+    a.n_tiles = paged_tile_numbers(n_rows, n_seq);
     a.n_items = 2 * a.n_tiles * n_heads;
     a.ld_token = ld_token; a.ld_head = ld_head;
     a.consts = ds->consts; a.S = ds->S_f32;

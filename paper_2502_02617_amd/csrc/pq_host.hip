@@ -322,16 +322,22 @@ void build_exact(const pq_ctx *ctx, PqExact &e)
     e.tan1[1] = 1.0;
     e.tan1[2] = tan(3.0 * kPi / 8.0);
     for (int k = 0; k < 15; ++k) e.pseudo1[k] = pseudo_angle(ctx->boundaries[0][k + 1]);
+    e.pseudo1_f[0] = 0.f;
+    e.pseudo1_f[16] = 4.f;
+    for (int k = 0; k < 15; ++k) e.pseudo1_f[k + 1] = (float)e.pseudo1[k];
+    auto weight = [](double t) { return (float)(1.0 / (sin(t) * (1.0 + tan(t)))); };
     for (int l = 0; l < 3; ++l) {
         for (int k = 0; k < 3; ++k) {
             const double t = tan(ctx->boundaries[l + 1][k + 1]);
             e.tan2[l][k] = t * t;
+            e.doubt[l][k] = weight(ctx->boundaries[l + 1][k + 1]);
         }
         if (!ctx->general_codebooks) e.tan2[l][1] = 1.0; /* pi/4 by symmetry of the density */
         if (ctx->depth == 7)
             for (int k = 0; k < (1 << ctx->upper_bits[l]) - 1; ++k) {
                 const double t = tan(ctx->upper_boundaries[l][k + 1]);
                 e.up_tan2[l][k] = t * t;
+                e.up_doubt[l][k] = weight(ctx->upper_boundaries[l][k + 1]);
             }
     }
 }

@@ -67,6 +67,35 @@ __device__ __forceinline__ int paged_find(int n, int64_t value, int lane, At sta
     return __builtin_amdgcn_readfirstlane(cnt) - 1;
 }
 
+/* A page with rows: its slot tau is row row0 + tau, as far as that is in [lo, hi), and token token0 + tau of its sequence.
+ * page -1: the sequence has none there. */
+struct PagedTile {
+    int64_t page, row0, lo, hi, token0;
+};
+
+/* The tiles of sequence b that hold rows are numbered from row_start[b] / 64 + 2 b on -- n rows that begin anywhere in a tile lie
+ * in n / 64 + 2 tiles at most, so the ranges do not meet, and no running sum has to be built first.  Numbers run below paged_tile_numbers;
+ * those without a tile have no rows (lo == hi).  All lanes of the wavefront take part. */
+static inline int64_t paged_tile_numbers(int64_t n_rows, int n_seq) { return n_rows / 64 + 2 * (int64_t)n_seq; }
+
+__device__ __forceinline__ PagedTile paged_tile(const PagedTable &t, const PagedRows &r, int64_t u, int lane)
+{
+    PagedTile p{-1, 0, 0, 0, 0};
+    auto offset = [&](int i) { return (int64_t)(max(r.row_start[i], 0) >> 6) + 2 * i; };
+    const int b = paged_find(r.n_seq, u, lane, offset);
+    if (b < 0 || b >= r.n_seq) return p;
+    const int64_t end = r.row_start[b + 1], n = end - r.row_start[b], ctx = r.ctx_len[b];
+    const int64_t first = max(ctx - n, (int64_t)0);
+    const int64_t t0 = ((first >> 6) + (u - offset(b))) * 64;
+    if (n <= 0 || t0 >= ctx) return p;
+    p.page = paged_page(t, b, t0);
+    p.row0 = end - ctx + t0;
+    p.lo = max(end - ctx + first, (int64_t)0);
+    p.hi = min(end, r.n_rows);
+    p.token0 = t0;
+    return p;
+}
+
 /* Where coordinate j of a rotated vector comes from: x_j cos + sign x_partner sin, entries `at` of the two halves of a table row.
  * Pairs are (2 i, 2 i + 1) or (i, i + dim / 2). */
 struct RotaryPair {

@@ -144,6 +144,37 @@ def test_append(name, batch):
         assert np.array_equal(now[:, untouched], before_it[:, untouched])
 
 
+@pytest.mark.parametrize("name", FORMATS)
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_append_in_chunks_and_one_by_one(name, dtype):
+    """Codes do not depend on the batch a vector comes in: 20000 tokens of two sequences as chunks and as 20000 rows of their own.  Radii may differ by a
+    rounding, as everywhere, one in a thousand of them at most."""
+    f, rng = fmt(name), np.random.default_rng(3)
+    n, heads = 20000, 2
+    lens, new = [n // 2 + 37, n // 2 + 5], [n // 2, n // 2]
+    n_pages = sum((m + 63) // 64 for m in lens)
+    pages = paged_ref.page_table(rng, n_pages, lens)
+    xk, xv = rows(rng, n, heads, dtype)
+    if name == "identity":      # coordinates that differ, so that none lies on a cell border
+        xk, xv = (xk.float() + torch.rand(xk.shape, device=DEV) * 1e-3 for _ in range(2)) if dtype == torch.float32 else (xk, xv)
+    rot = Rotary(torch.from_numpy(paged_ref.cos_sin(n, 128)).to(DEV))
+    caches = [paged_ref.Cache(f, heads, n_pages, fill=0) for _ in range(2)]
+    f.ctx.append_paged(xk, xv, dev32(np.cumsum([0] + new)), dev32(lens), *caches[0].all, dev32(pages), rotary=rot)
+    token = np.concatenate([np.arange(m - k, m) for m, k in zip(lens, new)])
+    each = np.repeat(pages, new, axis=0)
+    f.ctx.append_paged(xk, xv, dev32(np.arange(n + 1)), dev32(token + 1), *caches[1].all, dev32(each), rotary=rot)
+    torch.cuda.synchronize()
+    a, b = caches
+    assert torch.equal(a.kc, b.kc) and torch.equal(a.vc, b.vc)
+    for x, y in ((a.kr, b.kr), (a.vr, b.vr)):
+        if f.bits:      # words of a radius and codes
+            x, y = x.view(torch.int32), y.view(torch.int32)
+            assert torch.equal(x & 0xFFFF, y & 0xFFFF)
+            x, y = x >> 16, y >> 16
+        step = (x.int() - y.int()).abs()
+        assert int(step.max()) <= 1 and float((step > 0).float().mean()) <= 1e-3
+
+
 @pytest.mark.parametrize("name", ["general", "deep"])
 def test_append_positions_without_table_and_rows_of_nobody(name):
     """Given positions; no rotation; tokens without a page, negative tokens and rows behind the last sequence write nothing."""
