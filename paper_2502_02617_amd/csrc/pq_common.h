@@ -76,10 +76,10 @@ struct PqExact {
     double pseudo1[15];    /* general codebooks: pseudo-angles of the inner boundaries of level 1 (PqDeviceConsts::lut1) */
     double tan2[3][3];     /* squared tangents of the inner boundaries of levels 2, 3, 4 */
     double up_tan2[3][7];  /* the same of levels 5, 6, 7 (depth 7) */
-    /* Which codes 32 bits leave in doubt (paged append of whole tiles): weights that make the distances of a node's inputs from its
-       boundaries comparable, 1 / (sin t (1 + tan t)) of boundary t of levels 2, 3, 4 and 5, 6, 7, and the inner boundaries' pseudo-angles
-       of level 1 between 0 and 4. */
-    float doubt[3][3], up_doubt[3][7];
+    /* Which codes 32 bits leave in doubt (paged append of whole tiles): the largest sin t (1 + tan t) of a level's boundaries t -- how far
+       a comparison of squares moves with its inputs -- of levels 2, 3, 4 and 5, 6, 7, and the boundaries' pseudo-angles of level 1 between
+       0 and 4. */
+    float doubt[6];
     float pseudo1_f[17];
 };
 
@@ -87,6 +87,8 @@ struct PqExact {
 struct PqDeviceState {
     bool ready = false;
     PqExact *exact = nullptr;         /* device */
+    uint16_t *S_f16x2 = nullptr;      /* device: 2^15 S as two binary16 terms, or +-1 and zero if its entries are all +-1/sqrt(d); in the order of
+                                         S_bf16x3 */
     PqDeviceConsts *consts = nullptr; /* device */
     float *S_f32 = nullptr;           /* device [128][128], S[i][j]              */
     float *St_f32 = nullptr;          /* device [128][128], St[j][i] = S[i][j]   */

@@ -325,19 +325,19 @@ void build_exact(const pq_ctx *ctx, PqExact &e)
     e.pseudo1_f[0] = 0.f;
     e.pseudo1_f[16] = 4.f;
     for (int k = 0; k < 15; ++k) e.pseudo1_f[k + 1] = (float)e.pseudo1[k];
-    auto weight = [](double t) { return (float)(1.0 / (sin(t) * (1.0 + tan(t)))); };
+    auto moves = [&](float &most, double t) { most = fmaxf(most, (float)(sin(t) * (1.0 + tan(t)))); };
     for (int l = 0; l < 3; ++l) {
         for (int k = 0; k < 3; ++k) {
             const double t = tan(ctx->boundaries[l + 1][k + 1]);
             e.tan2[l][k] = t * t;
-            e.doubt[l][k] = weight(ctx->boundaries[l + 1][k + 1]);
+            moves(e.doubt[l], ctx->boundaries[l + 1][k + 1]);
         }
         if (!ctx->general_codebooks) e.tan2[l][1] = 1.0; /* pi/4 by symmetry of the density */
         if (ctx->depth == 7)
             for (int k = 0; k < (1 << ctx->upper_bits[l]) - 1; ++k) {
                 const double t = tan(ctx->upper_boundaries[l][k + 1]);
                 e.up_tan2[l][k] = t * t;
-                e.up_doubt[l][k] = weight(ctx->upper_boundaries[l][k + 1]);
+                moves(e.doubt[3 + l], ctx->upper_boundaries[l][k + 1]);
             }
     }
 }
@@ -581,6 +581,7 @@ extern "C" void pq_destroy(pq_ctx *ctx)
         if (hipSetDevice(i) != hipSuccess) continue;
         (void)hipFree(s.consts);
         (void)hipFree(s.exact);
+        (void)hipFree(s.S_f16x2);
         (void)hipFree(s.S_f32);
         (void)hipFree(s.St_f32);
         (void)hipFree(s.S_bf16x3);
@@ -607,7 +608,7 @@ pq_status pq_device_state(const pq_ctx *cctx, const PqDeviceState **out)
             }
         /* S = S1 + S2 + S3 with bf16 terms (24 significant bits in total), stored in
            the order the encode kernel's matrix-core A operand consumes them. */
-        std::vector<uint16_t> sb((size_t)3 * PQ_SB_TERM_STRIDE);
+        std::vector<uint16_t> sb((size_t)3 * PQ_SB_TERM_STRIDE), sh((size_t)2 * PQ_SB_TERM_STRIDE);
         for (int rt = 0; rt < 4; ++rt)
             for (int ks = 0; ks < 8; ++ks)
                 for (int lane = 0; lane < 64; ++lane)
@@ -629,15 +630,20 @@ pq_status pq_device_state(const pq_ctx *cctx, const PqDeviceState **out)
                         sb[at] = t1;
                         sb[PQ_SB_TERM_STRIDE + at] = t2;
                         sb[2 * (size_t)PQ_SB_TERM_STRIDE + at] = t3;
+                        if (!ctx->unit_entries) v *= 0x1p15;
+                        const _Float16 h1 = (_Float16)v, h2 = (_Float16)(v - (double)h1);
+                        memcpy(&sh[at], &h1, 2);
+                        memcpy(&sh[PQ_SB_TERM_STRIDE + at], &h2, 2);
                     }
         std::vector<PqExact> exact(1);
         build_exact(ctx, exact[0]);
         PqDeviceState t;
         auto release = [&t]() { /* a failed set-up leaves nothing behind: the next call starts over */
-            (void)hipFree(t.consts); (void)hipFree(t.exact); (void)hipFree(t.S_f32); (void)hipFree(t.St_f32); (void)hipFree(t.S_bf16x3);
+            (void)hipFree(t.consts); (void)hipFree(t.exact); (void)hipFree(t.S_f16x2); (void)hipFree(t.S_f32); (void)hipFree(t.St_f32); (void)hipFree(t.S_bf16x3);
         };
         if (hipMalloc((void **)&t.consts, sizeof(PqDeviceConsts)) != hipSuccess ||
             hipMalloc((void **)&t.exact, sizeof(PqExact)) != hipSuccess ||
+            hipMalloc((void **)&t.S_f16x2, sh.size() * 2) != hipSuccess ||
             hipMalloc((void **)&t.S_f32, Sf.size() * 4) != hipSuccess ||
             hipMalloc((void **)&t.St_f32, Stf.size() * 4) != hipSuccess ||
             hipMalloc((void **)&t.S_bf16x3, sb.size() * 2) != hipSuccess) {
@@ -646,6 +652,7 @@ pq_status pq_device_state(const pq_ctx *cctx, const PqDeviceState **out)
         }
         if (hipMemcpy(t.consts, &ctx->host_consts, sizeof(PqDeviceConsts), hipMemcpyHostToDevice) != hipSuccess ||
             hipMemcpy(t.exact, exact.data(), sizeof(PqExact), hipMemcpyHostToDevice) != hipSuccess ||
+            hipMemcpy(t.S_f16x2, sh.data(), sh.size() * 2, hipMemcpyHostToDevice) != hipSuccess ||
             hipMemcpy(t.S_f32, Sf.data(), Sf.size() * 4, hipMemcpyHostToDevice) != hipSuccess ||
             hipMemcpy(t.St_f32, Stf.data(), Stf.size() * 4, hipMemcpyHostToDevice) != hipSuccess ||
             hipMemcpy(t.S_bf16x3, sb.data(), sb.size() * 2, hipMemcpyHostToDevice) != hipSuccess) {

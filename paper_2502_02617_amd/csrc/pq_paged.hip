@@ -47,6 +47,23 @@ __device__ __forceinline__ PagedPlace paged_place(const AppendPagedArgs &a, int6
     return p;
 }
 
+/* The boundaries that settle codes, requested ahead of the vector they are for. */
+struct ExactBounds {
+    double tan1[3], tan2[3][3];
+    bool general, deep;
+    __device__ __forceinline__ void load(const PqExact &E, const PqDeviceConsts &K)
+    {
+#pragma unroll
+        for (int k = 0; k < 3; ++k) {
+            tan1[k] = E.tan1[k];
+#pragma unroll
+            for (int l = 0; l < 3; ++l) tan2[l][k] = E.tan2[l][k];
+        }
+        general = K.general != 0;
+        deep = K.depth == 7;
+    }
+};
+
 /* procedure Quant inside a quadrant, in 64 bits: boundaries below atan(v / u), u, v >= 0 (or of squares, with squared tangents) */
 __device__ __forceinline__ uint32_t quant3_exact(double u, double v, const double (&t)[3])
 {
@@ -61,11 +78,11 @@ __device__ __forceinline__ uint32_t quant_upper_exact(double u2, double v2, cons
 }
 
 /* level-1 code of (ya, yb): quadrant from the signs and the cell inside it, or the number of boundaries below its pseudo-angle */
-__device__ __forceinline__ uint32_t level1_exact(double ya, double yb, const PqExact &E, bool general)
+__device__ __forceinline__ uint32_t level1_exact(double ya, double yb, const PqExact &E, const ExactBounds &B)
 {
     const uint32_t sa = (uint32_t)(__double2hiint(ya)) >> 31, sb = (uint32_t)(__double2hiint(yb)) >> 31, f = sa ^ sb;
     const double a = fabs(ya), b = fabs(yb);
-    if (!general) return (quant3_exact(a, b, E.tan1) ^ (f ? 7u : 0u)) | (sb << 3);
+    if (!B.general) return (quant3_exact(a, b, B.tan1) ^ (f ? 7u : 0u)) | (sb << 3);
     const double sum = a + b;
     const double p = (double)(2u * sb + f) + (sum > 0.0 ? (f ? a : b) / sum : 0.0);
     uint32_t c = 0;
@@ -88,19 +105,19 @@ __device__ __forceinline__ double shfl_xor_double(double x, int d)
 /* One rotated vector, coordinates 2 p and 2 p + 1 in lane p, to slot tau of a page: the recursion of procedure Polar with the codes'
  * comparisons, the nodes above level 1 in the lanes of their first leaf (the others compute the same along). */
 template <int KIND>
-__device__ __forceinline__ void write_exact(const AppendPagedArgs &a, double ya, double yb, int64_t tile, int tau, int lane)
+__device__ __forceinline__ void write_exact(const AppendPagedArgs &a, const ExactBounds &B, double ya, double yb, int64_t tile, int tau, int lane)
 {
     const PqExact &E = *a.exact;
     const PqDeviceConsts &K = *a.consts;
     const int i = lane & 7, b = lane >> 3;
-    const uint32_t code1 = level1_exact(ya, yb, E, K.general != 0);
+    const uint32_t code1 = level1_exact(ya, yb, E, B);
     const double q1 = ya * ya + yb * yb, q1s = shfl_xor_double(q1, 1);
-    const uint32_t c2 = quant3_exact(q1, q1s, E.tan2[0]);
+    const uint32_t c2 = quant3_exact(q1, q1s, B.tan2[0]);
     const double q2 = q1 + q1s, q2s = shfl_xor_double(q2, 2);
-    const uint32_t c3 = quant3_exact(q2, q2s, E.tan2[1]);
+    const uint32_t c3 = quant3_exact(q2, q2s, B.tan2[1]);
     const double q3 = q2 + q2s, q3s = shfl_xor_double(q3, 4);
     PqBlockFields f;
-    f.c4 = quant3_exact(q3, q3s, E.tan2[2]);
+    f.c4 = quant3_exact(q3, q3s, B.tan2[2]);
     const double q4 = q3 + q3s;
     f.radius = radius_exact(q4);
     /* level-1 codes at their nibbles; [c2(2h) | c3(h) | c2(2h+1)] of half-block h at bits [8 h, 8 h + 6) */
@@ -116,9 +133,9 @@ __device__ __forceinline__ void write_exact(const AppendPagedArgs &a, double ya,
     f.g6[1] = (gw >> 8) & 63u;
     if (i == 0) {
         pql_put_block<true>(reinterpret_cast<uint32_t *>(a.codes[KIND] + tile * PQL_CODE_BYTES), KIND, tau, b, f);
-        if (K.depth != 7) a.radii[KIND][tile * PQL_RADII + pql_pos(KIND, tau, b).radius_half] = f.radius;
+        if (!B.deep) a.radii[KIND][tile * PQL_RADII + pql_pos(KIND, tau, b).radius_half] = f.radius;
     }
-    if (K.depth == 7) { /* levels 5, 6, 7 over the block radii, and the vector's word of the radius plane */
+    if (B.deep) { /* levels 5, 6, 7 over the block radii, and the vector's word of the radius plane */
         const int b5 = K.up_bits[0], b6 = K.up_bits[1], b7 = K.up_bits[2];
         const double q4s = shfl_xor_double(q4, 8), q5 = q4 + q4s;
         const uint32_t c5 = quant_upper_exact(q4, q4s, E.up_tan2[0], (1 << b5) - 1);
@@ -198,6 +215,8 @@ __device__ __forceinline__ void append_vectors_exact(const AppendPagedArgs &a, i
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     ExactSlice s;
     s.load(a.exact->S, tid);
+    ExactBounds bounds;
+    bounds.load(*a.exact, *a.consts);
     const int r = min(wave >> 1, NV - 1); /* a vector beyond the range repeats the last one and is not written */
     const int64_t vec = min(vec0 + r, n_vec - 1), row = vec / a.n_heads;
     const int head = (int)(vec - row * a.n_heads);
@@ -208,7 +227,7 @@ __device__ __forceinline__ void append_vectors_exact(const AppendPagedArgs &a, i
     multiply_exact<NV>(s, lds, tid);
     __syncthreads();
     if ((wave & 1) == 0 && (wave >> 1) < NV && vec0 + r < n_vec && at.page >= 0)
-        write_exact<KIND>(a, rotated_exact(lds, r, 2 * lane), rotated_exact(lds, r, 2 * lane + 1), head * a.table.pool_pages + at.page, at.tau, lane);
+        write_exact<KIND>(a, bounds, rotated_exact(lds, r, 2 * lane), rotated_exact(lds, r, 2 * lane + 1), head * a.table.pool_pages + at.page, at.tau, lane);
 }
 
 /* workgroups [0, n_blocks): keys, the rest: values */
@@ -225,14 +244,17 @@ __global__ __launch_bounds__(512) void pq_append_paged_kernel(AppendPagedArgs a,
  * A workgroup per tile, as for short inputs of pq_encode_kv: rows are rotated in fp32 and left in LDS as matrix operands, eight threads
  * per vector; wavefront (v, rt) multiplies the 32 vectors of half v into row tile rt of S and runs the recursion of blocks rt and 4 + rt.
  *
- * Codes in doubt.  A rotated coordinate is off by E = 2^-22 |x| at most (derivation and measurement at kDoubt), so the code of a node is
- * certain if its inputs u, v are further from every boundary t than that: |tan t u - v| > (1 + tan t) E at level 1, and above it, where
- * squares are compared, |tan^2 t u^2 - v^2| > 2 sqrt 2 E |(u, v)| sin t (1 + tan t).  The square root is bounded from above by
- * (q / s + s) / 2, q = u^2 + v^2, with s the node's usual radius; doubt is therefore only ever found too often.  Of
- * vectors without a preferred direction 1 in 250 has a code in doubt; the workgroup marks them and, behind its last tile, codes them once more in
- * 64 bits, four at a time. */
+ * Codes in doubt.  A rotated coordinate is off by less than E = 2^-22 |x|: 24 products of matrix instructions add to one fp32 sum, whose
+ * roundings are 2^-24 of partial sums far below |x|; with 2^-24 in place of 2^-22 no code of 2 * 10^9 was wrong, with 2^-26 13 were, and
+ * without any doubt 326.  The code of a node is certain if its inputs u, v are further from every boundary t than that moves the
+ * comparison: |tan t u - v| > (1 + tan t) E at level 1, where a coordinate's sign is a boundary as well; above it, where squares are
+ * compared, |tan^2 t u^2 - v^2| > 2 sqrt 2 E |(u, v)| sin t (1 + tan t).  The largest factor of a level's boundaries serves for all, and
+ * |(u, v)| is bounded from above by (q / s + s) / 2, q = u^2 + v^2, with s the node's usual radius: doubt is only ever found too often, in 1 of
+ * 250 vectors without a preferred direction.  The workgroup lists them and, behind its last tile, codes them once more in 64 bits, four
+ * at a time. */
 constexpr float kDoubt = 0x1p-22f;
-constexpr int kChunkItems = 512; /* tiles of one workgroup at most */
+constexpr int kChunkItems = 256; /* tiles of one workgroup at most */
+constexpr int kListed = 256;     /* vectors that are coded once more in one go */
 
 struct ChunkItem { /* a tile that the workgroup has written */
     int32_t page, row0, token0, head_kind;
@@ -240,87 +262,109 @@ struct ChunkItem { /* a tile that the workgroup has written */
 
 /* what the certainty of a vector's codes is measured with */
 struct Doubt {
-    float e;          /* E */
+    float e;          /* level 1: (1 + tan 3 pi / 8) E */
     float b2, b3, b4; /* the vector's part of the bounds of levels 2, 3, 4 */
 };
 
-/* 2 sqrt 2 E (q / s + s) / 2 = c q + b |x|^2 with s = rho |x|, a node's radius among 128 coordinates; and 2^-21 q for the roundings of the
-   squares and their sums */
-template <int LEVEL>
-__device__ __forceinline__ constexpr float doubt_rho() { return LEVEL == 2 ? 0.1767767f : (LEVEL == 3 ? 0.25f : 0.3535534f); }
+/* What a level's bound is made of: 2 sqrt 2 E f (q / s + s) / 2 = c q + b |x|^2 with s = rho |x|, a node's radius among 128 coordinates, f the
+   level's factor (PqExact::doubt); and 2^-21 q for the roundings of the squares and their sums. */
+struct DoubtLevels {
+    float c2, c3, c4, b2, b3, b4;
+};
 
-__device__ __forceinline__ Doubt doubt_of(float norm2)
+__device__ __forceinline__ DoubtLevels doubt_levels(const PqExact &E)
 {
-    const float k = 1.4142136f * kDoubt * norm2;
-    return Doubt{kDoubt * __builtin_amdgcn_sqrtf(norm2), k * doubt_rho<2>(), k * doubt_rho<3>(), k * doubt_rho<4>()};
+    constexpr float kRho2 = 0.1767767f, kRho3 = 0.25f, kRho4 = 0.3535534f, k = 1.4142136f * kDoubt;
+    return DoubtLevels{__builtin_fmaf(E.doubt[0], k / kRho2, 0x1p-21f), __builtin_fmaf(E.doubt[1], k / kRho3, 0x1p-21f),
+                       __builtin_fmaf(E.doubt[2], k / kRho4, 0x1p-21f), E.doubt[0] * (k * kRho2), E.doubt[1] * (k * kRho3), E.doubt[2] * (k * kRho4)};
+}
+
+__device__ __forceinline__ Doubt doubt_of(float norm2, const DoubtLevels &l)
+{
+    return Doubt{3.4142136f * kDoubt * __builtin_amdgcn_sqrtf(norm2), norm2 * l.b2, norm2 * l.b3, norm2 * l.b4};
 }
 
 __device__ __forceinline__ float min3_abs(float a, float b, float c) { return fminf(fminf(fabsf(a), fabsf(b)), fabsf(c)); }
 
-/* distance of a node above level 1 from its nearest boundary, less what it may be off */
-template <int LEVEL>
-__device__ __forceinline__ float doubt_node(float u, float v, float t1, float t2, float t3, const float (&w)[3], float b)
+/* distance of a node above level 1 from its nearest boundary, less the node's part of what it may be off */
+__device__ __forceinline__ float doubt_node(float u, float v, float t1, float t2, float t3, float c)
 {
-    constexpr float c = 1.4142136f * kDoubt / doubt_rho<LEVEL>() + 0x1p-21f;
-    const float d = min3_abs(__builtin_fmaf(t1, u, -v) * w[0], __builtin_fmaf(t2, u, -v) * w[1], __builtin_fmaf(t3, u, -v) * w[2]);
-    return __builtin_fmaf(-c, u + v, d) - b;
+    return __builtin_fmaf(-c, u + v, min3_abs(__builtin_fmaf(t1, u, -v), __builtin_fmaf(t2, u, -v), __builtin_fmaf(t3, u, -v)));
 }
 
-/* polar_quant_block, and whether a code is in doubt.  The weights of level 1 are 1 / (1 + tan t); a coordinate's sign is a boundary as well. */
+/* polar_quant_block, and whether a code is in doubt */
 template <bool GENERAL>
-__device__ __forceinline__ BlockCodes quant_block_checked(const f32x16 &y, const Thresholds &th, const Doubt &d, const float (&w)[3][3], const float *pseudo,
+__device__ __forceinline__ BlockCodes quant_block_checked(const f32x16 &y, const Thresholds &th, const Doubt &d, const DoubtLevels &l, const float *pseudo,
                                                           bool &doubt)
 {
     PolarState s;
-    float near1 = INFINITY, near = INFINITY;
+    float near1 = INFINITY, near2 = INFINITY, near3 = INFINITY;
     const float t2b = GENERAL ? th.t2b : 1.f, t3b = GENERAL ? th.t3b : 1.f, t4b = GENERAL ? th.t4b : 1.f;
 #pragma unroll
     for (int p = 0; p < 8; ++p) {
         polar_level1_a<GENERAL>(s, y, p, th);
+        const float a = fabsf(y[2 * p]), b = fabsf(y[2 * p + 1]);
         if (GENERAL) {
-            /* pseudo-angle: off by 2 E / (|a| + |b|) and a rounding of numbers below 4 */
-            const float a = fabsf(y[2 * p]), b = fabsf(y[2 * p + 1]), sum = a + b;
+            /* pseudo-angle: off by 2 E / (a + b) and a rounding of numbers below 4 */
+            const float sum = a + b;
             const uint32_t ba = __float_as_uint(y[2 * p]), bb = __float_as_uint(y[2 * p + 1]), sb = bb >> 31, f = (ba ^ bb) >> 31;
             const float pa = (float)(2u * sb + f) + (sum > 0.f ? (f ? a : b) * __builtin_amdgcn_rcpf(sum) : 0.f);
             const float gap = fminf(pa - pseudo[s.mq], pseudo[s.mq + 1] - pa);
-            near1 = fminf(near1, __builtin_fmaf(gap - 0x1p-20f, sum, -4.f * d.e));
+            near1 = fminf(near1, (gap - 0x1p-20f) * sum);
         } else {
-            const float a = fabsf(y[2 * p]), b = fabsf(y[2 * p + 1]);
-            const float dist = min3_abs(__builtin_fmaf(th.t1a, a, -b) * 0.70710678f, (a - b) * 0.5f, __builtin_fmaf(th.t1c, a, -b) * 0.29289322f);
-            near1 = fminf(near1, fminf(dist, fminf(a, b)) - d.e);
+            near1 = fminf(fminf(near1, fminf(a, b)), min3_abs(__builtin_fmaf(th.t1a, a, -b), a - b, __builtin_fmaf(th.t1c, a, -b)));
         }
         polar_level1_b<GENERAL>(s, y, p);
         polar_upper<GENERAL>(s, p, th);
         if (p & 1) {
             const int n = p >> 1;
-            near = fminf(near, doubt_node<2>(s.q1[2 * n], s.q1[2 * n + 1], th.t2a, t2b, th.t2c, w[0], d.b2));
+            near2 = fminf(near2, doubt_node(s.q1[2 * n], s.q1[2 * n + 1], th.t2a, t2b, th.t2c, l.c2));
         }
         if ((p & 3) == 3) {
             const int h = p >> 2;
-            near = fminf(near, doubt_node<3>(s.q2[2 * h], s.q2[2 * h + 1], th.t3a, t3b, th.t3c, w[1], d.b3));
+            near3 = fminf(near3, doubt_node(s.q2[2 * h], s.q2[2 * h + 1], th.t3a, t3b, th.t3c, l.c3));
         }
     }
-    near = fminf(near, doubt_node<4>(s.q3[0], s.q3[1], th.t4a, t4b, th.t4c, w[2], d.b4));
-    doubt = near1 < 0.f || near < 0.f;
+    const float near4 = doubt_node(s.q3[0], s.q3[1], th.t4a, t4b, th.t4c, l.c4);
+    doubt = near1 < d.e || near2 < d.b2 || near3 < d.b3 || near4 < d.b4;
     return s.out;
 }
 
 /* the same of a node of levels 5, 6, 7 */
-__device__ __forceinline__ bool upper_in_doubt(float u2, float v2, const float *tan2, const float *w, int n_bounds, float e)
+__device__ __forceinline__ bool upper_in_doubt(float u2, float v2, const float *tan2, float factor, int n_bounds, float e)
 {
-    const float q = u2 + v2, bound = 2.8284271f * e * __builtin_amdgcn_sqrtf(q) + 0x1p-20f * q;
+    const float q = u2 + v2, bound = 2.8284271f * factor * e * __builtin_amdgcn_sqrtf(q) + 0x1p-20f * q;
     bool doubt = false;
 #pragma unroll
     for (int k = 0; k < 7; ++k)
-        if (k < n_bounds) doubt |= fabsf(__builtin_fmaf(tan2[k], u2, -v2)) * w[k] < bound;
+        if (k < n_bounds) doubt |= fabsf(__builtin_fmaf(tan2[k], u2, -v2)) < bound;
     return doubt;
+}
+
+/* maximum and sum over the eight lanes lane & 7 + 8 k */
+__device__ __forceinline__ float over_parts_max(float x)
+{
+    x = fmaxf(x, pq_dpp<0x128>(x)); /* row_ror:8 */
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    x = fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+    const auto t = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return fmaxf(__uint_as_float(t[0]), __uint_as_float(t[1]));
+}
+
+__device__ __forceinline__ float over_parts_sum(float x)
+{
+    x += pq_dpp<0x128>(x);
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    x = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+    const auto t = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return __uint_as_float(t[0]) + __uint_as_float(t[1]);
 }
 
 template <int XT, int NTERMS, bool GENERAL, bool DEEP>
 __global__ __launch_bounds__(512) void pq_append_chunk_kernel(AppendPagedArgs a, const uint4 *S_terms, int64_t n_items)
 {
     typedef Operands<PQ_F32, NTERMS> Op; /* rotated rows are fp32, whatever the input's type */
-    constexpr int NXT = Op::x_terms, kIn = NTERMS == 1 ? 1 : 3, kThreads = 512;
+    constexpr int NXT = Op::x_terms, kThreads = 512;
     constexpr int kImgDwords = TileImage<DEEP>::dwords, kRadiiHalves = TileImage<DEEP>::radii_halves;
     constexpr int kRows = NXT * 8 * 2 * 64; /* a tile's rows, [term][k-step][half][lane] */
     constexpr int kRaw = XT == PQ_BF16 ? 2 : 4;
@@ -335,72 +379,85 @@ __global__ __launch_bounds__(512) void pq_append_chunk_kernel(AppendPagedArgs a,
     __shared__ float sPseudo[17];
     __shared__ ChunkItem sItem[kChunkItems];
     __shared__ uint32_t sDoubt[kChunkItems][2];
-    __shared__ uint32_t sList[256];
+    __shared__ uint32_t sList[kListed];
     __shared__ int sCount;
+    /* the rotation table's rows of a tile's tokens: a tile's heads follow each other.  Rows of 132: the eight vectors of a wavefront then
+       begin on different banks. */
+    __shared__ __align__(16) float sTurn[64][132];
     const int tid = threadIdx.x, lane = tid & 63, j = lane & 31, H = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), v = wave & 1, rt = wave >> 1;
-    const int64_t item_end = (int64_t)(blockIdx.x + 1) * n_items / gridDim.x;
-
     /* items: tile numbers, for each the keys of all heads, then the values: a workgroup has consecutive ones, so a tile's place is looked
        up once for many of them and its rotation table's rows stay near */
-    struct Item {
-        int64_t index; /* item_end: none */
-        int kind, head;
-        PagedTile t;
-    };
     const int per_tile = 2 * a.n_heads;
-    auto find = [&](int64_t index, const Item &from) { /* the first item from `index` on that has something to write */
-        Item it = from;
-        int64_t u = index / per_tile;
-        bool known = from.index < item_end && from.index >= 0 && from.index / per_tile == u;
-        while (index < item_end) {
-            if (!known) it.t = paged_tile(a.table, a.rows, u, lane);
-            if (it.t.page >= 0 && it.t.lo < it.t.hi) break;
-            known = false;
-            ++u;
-            index = u * per_tile;
+    struct Item {
+        int u, rest;                /* tile number, item of the tile */
+        int page, row0, lo, hi;     /* slots [lo, hi) are written, slot tau from row row0 + tau */
+        int token0;
+        int some;                   /* 0: behind the last (an int: the padding behind a bool is copied through memory) */
+    };
+    const int64_t first_item = (int64_t)blockIdx.x * n_items / gridDim.x, item_end = (int64_t)(blockIdx.x + 1) * n_items / gridDim.x;
+    const int u_end = (int)(item_end / per_tile), rest_end = (int)(item_end % per_tile);
+    auto look_up = [&](Item &it) { /* from item (u, rest) on, the next one that has something to write */
+        for (;;) {
+            it.some = it.u < u_end || (it.u == u_end && it.rest < rest_end);
+            if (!it.some) return;
+            const PagedTile t = paged_tile(a.table, a.rows, it.u, lane);
+            if (t.page >= 0 && t.lo < t.hi) {
+                it.page = (int)t.page;
+                it.row0 = (int)t.row0;
+                it.lo = (int)max(t.lo - t.row0, (int64_t)0);
+                it.hi = (int)min(t.hi - t.row0, (int64_t)64);
+                it.token0 = (int)t.token0;
+                return;
+            }
+            ++it.u;
+            it.rest = 0;
         }
-        it.index = index < item_end ? index : item_end;
-        const int rest = (int)(it.index - u * per_tile);
-        it.kind = rest >= a.n_heads ? PQ_VALUE : PQ_KEY;
-        it.head = rest - (rest >= a.n_heads ? a.n_heads : 0);
+    };
+    auto following = [&](const Item &from) {
+        Item it = from;
+        if (++it.rest == per_tile) {
+            it.rest = 0;
+            ++it.u;
+            look_up(it);
+        } else {
+            it.some = it.u < u_end || (it.u == u_end && it.rest < rest_end);
+        }
         return it;
     };
-    /* slots [tau_lo, tau_hi) of the tile are written */
-    auto tau_lo = [](const Item &it) { return (int)max(it.t.lo - it.t.row0, (int64_t)0); };
-    auto tau_hi = [](const Item &it) { return (int)min(it.t.hi - it.t.row0, (int64_t)64); };
+    auto kind_of = [&](const Item &it) { return it.rest >= a.n_heads ? PQ_VALUE : PQ_KEY; };
+    auto head_of = [&](const Item &it) { return it.rest >= a.n_heads ? it.rest - a.n_heads : it.rest; };
 
     /* this thread's sixteen coordinates 16 part .. + 15 of vector vec, in two pieces of eight; a slot that is not written gets the first row
        that is */
     const int vec = 8 * wave + (lane & 7), part = lane >> 3, half_dim = a.rot.dim >> 1;
     uint4 raw[kRaw], other[kRaw];
-    float4 co[4], si[4];
     auto load_row = [&](const Item &it) {
-        const int lo = tau_lo(it), slot = vec >= lo && vec < tau_hi(it) ? vec : lo;
-        const int64_t row = it.t.row0 + slot, off = row * a.ld_token + (int64_t)it.head * a.ld_head;
+        const int kind = kind_of(it);
+        const int64_t row = it.row0 + (vec >= it.lo && vec < it.hi ? vec : it.lo), off = row * a.ld_token + (int64_t)head_of(it) * a.ld_head;
         constexpr int kBytes = XT == PQ_BF16 ? 2 : 4;
-        const char *base = static_cast<const char *>(a.x[it.kind]) + off * kBytes;
+        const char *base = static_cast<const char *>(a.x[kind]) + off * kBytes;
 #pragma unroll
         for (int k = 0; k < kRaw; ++k) raw[k] = reinterpret_cast<const uint4 *>(base + 16 * part * kBytes)[k];
-        if (it.kind != PQ_KEY || 16 * part >= a.rot.dim) return;
-        const float *cs = rotary_row(a.rot, a.positions ? (int64_t)a.positions[row] : it.t.token0 + slot);
+        if (kind != PQ_KEY || 16 * part >= a.rot.dim || a.rot.interleaved) return;
 #pragma unroll
         for (int k = 0; k < 2; ++k) { /* dim is a multiple of 16, its half one of 8: a piece lies in one half of the pairs */
-            const int c = 16 * part + 8 * k;
-            if (a.rot.interleaved) {
-                co[2 * k] = *reinterpret_cast<const float4 *>(cs + c / 2);
-                si[2 * k] = *reinterpret_cast<const float4 *>(cs + half_dim + c / 2);
-            } else {
-                const int at = c < half_dim ? c : c - half_dim, partner = c < half_dim ? c + half_dim : c - half_dim;
+            const int c = 16 * part + 8 * k, partner = c < half_dim ? c + half_dim : c - half_dim;
 #pragma unroll
-                for (int q = 0; q < 2; ++q) {
-                    co[2 * k + q] = *reinterpret_cast<const float4 *>(cs + at + 4 * q);
-                    si[2 * k + q] = *reinterpret_cast<const float4 *>(cs + half_dim + at + 4 * q);
-                }
-#pragma unroll
-                for (int q = 0; q < kRaw / 2; ++q) other[(kRaw / 2) * k + q] = reinterpret_cast<const uint4 *>(base + partner * kBytes)[q];
-            }
+            for (int q = 0; q < kRaw / 2; ++q) other[(kRaw / 2) * k + q] = reinterpret_cast<const uint4 *>(base + partner * kBytes)[q];
         }
+    };
+    int turn_of = -1; /* the tile whose rows are in sTurn */
+    auto needs_turn = [&](const Item &it) { return a.rot.cs && it.some && kind_of(it) == PQ_KEY && it.u != turn_of; };
+    auto load_turn = [&](const Item &it) { /* all threads, and a barrier before and behind */
+        const int at = tid >> 3, slot = at >= it.lo && at < it.hi ? at : it.lo;
+        const float *cs = rotary_row(a.rot, a.positions ? (int64_t)a.positions[it.row0 + slot] : (int64_t)it.token0 + slot);
+        float4 t[4]; /* all requested before the first is stored; columns from dim on are nobody's */
+#pragma unroll
+        for (int k = 0; k < 4; ++k) t[k] = *reinterpret_cast<const float4 *>(cs + min(4 * (tid & 7) + 32 * k, a.rot.dim - 4));
+#pragma unroll
+        for (int k = 0; k < 4; ++k) *reinterpret_cast<float4 *>(&sTurn[at][4 * (tid & 7) + 32 * k]) = t[k];
+        turn_of = it.u;
     };
     auto floats = [](const uint4 *r, float (&f)[8]) {
         if constexpr (XT == PQ_BF16) {
@@ -420,8 +477,10 @@ __global__ __launch_bounds__(512) void pq_append_chunk_kernel(AppendPagedArgs a,
             floats(raw + (kRaw / 2) * k, f[k]);
             const int c = 16 * part + 8 * k;
             if (kind == PQ_KEY && c < a.rot.dim) {
+                const float *cs = &sTurn[vec][a.rot.interleaved ? c / 2 : (c < half_dim ? c : c - half_dim)];
+                const float4 c0 = *reinterpret_cast<const float4 *>(cs), s0 = *reinterpret_cast<const float4 *>(cs + half_dim);
+                const float cc[4] = {c0.x, c0.y, c0.z, c0.w}, ss[4] = {s0.x, s0.y, s0.z, s0.w};
                 if (a.rot.interleaved) {
-                    const float cc[4] = {co[2 * k].x, co[2 * k].y, co[2 * k].z, co[2 * k].w}, ss[4] = {si[2 * k].x, si[2 * k].y, si[2 * k].z, si[2 * k].w};
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
                         const float x = f[k][2 * e], y = f[k][2 * e + 1];
@@ -429,13 +488,16 @@ __global__ __launch_bounds__(512) void pq_append_chunk_kernel(AppendPagedArgs a,
                         f[k][2 * e + 1] = __builtin_fmaf(x, ss[e], y * cc[e]);
                     }
                 } else {
-                    const float cc[8] = {co[2 * k].x, co[2 * k].y, co[2 * k].z, co[2 * k].w, co[2 * k + 1].x, co[2 * k + 1].y, co[2 * k + 1].z, co[2 * k + 1].w};
-                    const float ss[8] = {si[2 * k].x, si[2 * k].y, si[2 * k].z, si[2 * k].w, si[2 * k + 1].x, si[2 * k + 1].y, si[2 * k + 1].z, si[2 * k + 1].w};
+                    const float4 c1 = *reinterpret_cast<const float4 *>(cs + 4), s1 = *reinterpret_cast<const float4 *>(cs + half_dim + 4);
+                    const float dd[4] = {c1.x, c1.y, c1.z, c1.w}, tt[4] = {s1.x, s1.y, s1.z, s1.w};
                     float o[8];
                     floats(other + (kRaw / 2) * k, o);
                     const float sign = c < half_dim ? -1.f : 1.f;
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) f[k][e] = __builtin_fmaf(f[k][e], cc[e], sign * (o[e] * ss[e]));
+                    for (int e = 0; e < 4; ++e) {
+                        f[k][e] = __builtin_fmaf(f[k][e], cc[e], sign * (o[e] * ss[e]));
+                        f[k][4 + e] = __builtin_fmaf(f[k][4 + e], dd[e], sign * (o[4 + e] * tt[e]));
+                    }
                 }
             }
         }
@@ -449,9 +511,7 @@ __global__ __launch_bounds__(512) void pq_append_chunk_kernel(AppendPagedArgs a,
             for (int k = 0; k < 2; ++k)
 #pragma unroll
                 for (int i = 0; i < 8; ++i) m = fmaxf(m, fabsf(f[k][i]));
-#pragma unroll
-            for (int d = 8; d < 64; d <<= 1) m = fmaxf(m, __shfl_xor(m, d)); /* the vector's eight parts */
-            e = half_exponent(m);
+            e = half_exponent(over_parts_max(m)); /* of the vector's eight parts */
             up = __uint_as_float(e << 23);
             if (part == 0) sUnscale[buffer][vec] = half_unscale<NTERMS>(e);
         }
@@ -463,8 +523,7 @@ __global__ __launch_bounds__(512) void pq_append_chunk_kernel(AppendPagedArgs a,
                 const float x = f[k][i] * up;
                 n2 = __builtin_fmaf(x, x, n2);
             }
-#pragma unroll
-        for (int d = 8; d < 64; d <<= 1) n2 += __shfl_xor(n2, d);
+        n2 = over_parts_sum(n2);
         /* |x|^2 as the products give it: with the 2^15 of two terms of S, or the sqrt(d) of entries +-1 */
         if (part == 0) sNorm2[buffer][vec] = n2 * (NTERMS == 2 ? 0x1p30f : (NTERMS == 1 ? 128.f : 1.f));
 #pragma unroll
@@ -477,53 +536,50 @@ __global__ __launch_bounds__(512) void pq_append_chunk_kernel(AppendPagedArgs a,
         }
     };
 
-    Item it{-1, 0, 0, {}};
-    it = find((int64_t)blockIdx.x * n_items / gridDim.x, it);
-    if (it.index >= item_end) return;
+    Item it{(int)(first_item / per_tile), (int)(first_item % per_tile), 0, 0, 0, 0, 0, 0};
+    look_up(it);
+    if (!it.some) return;
     load_row(it);
-    BOperand sa[8][NTERMS];
-    {
-        uint4 stage[8][kIn];
-#pragma unroll
-        for (int ks = 0; ks < 8; ++ks)
-#pragma unroll
-            for (int k = 0; k < kIn; ++k) stage[ks][k] = S_terms[((k * 4 + rt) * 8 + ks) * 64 + lane];
-        leave_row(0, it.kind);
-#pragma unroll
-        for (int ks = 0; ks < 8; ++ks) {
-            if (NTERMS == 2) __builtin_amdgcn_sched_barrier(0); /* one chunk after the other: all at once spills */
-            s_operand<PQ_F32, NTERMS>(sa[ks], stage[ks]);
-        }
+    if (needs_turn(it)) {
+        load_turn(it);
+        __syncthreads();
     }
+    BOperand sa[8][NTERMS]; /* requested behind the first rows */
+#pragma unroll
+    for (int ks = 0; ks < 8; ++ks)
+#pragma unroll
+        for (int k = 0; k < NTERMS; ++k) sa[ks][k].q = S_terms[((k * 4 + rt) * 8 + ks) * 64 + lane];
+    leave_row(0, kind_of(it));
     Thresholds th = load_thresholds(*a.consts, NTERMS == 1 ? PQ_INV_SQRT_D : 1.0f);
     const float base_scale = th.radius_scale;
     UpperTables ut = {};
     if (DEEP) ut = load_upper_tables(*a.consts);
-    float w[3][3];
-#pragma unroll
-    for (int l = 0; l < 3; ++l)
-#pragma unroll
-        for (int k = 0; k < 3; ++k) w[l][k] = a.exact->doubt[l][k];
+    const DoubtLevels levels = doubt_levels(*a.exact);
     if (GENERAL) {
         sLut[tid] = a.consts->lut1[tid];
         th.lut1 = sLut;
         if (tid < 17) sPseudo[tid] = a.exact->pseudo1_f[tid];
     }
     for (int i = tid; i < 2 * kChunkItems; i += kThreads) (&sDoubt[0][0])[i] = 0;
+    if (tid == 0) sCount = 0;
     const int tau = 32 * v + j;
-    Item next = find(it.index + 1, it);
-    if (next.index < item_end) load_row(next);
+    Item next = following(it);
+    if (next.some) load_row(next);
     __syncthreads();
+    if (needs_turn(next)) {
+        load_turn(next);
+        __syncthreads();
+    }
     int n_done = 0;
     /* buffers are used in turn: what a wavefront writes for the tile after the next is behind the next tile's barrier */
     for (int turn = 0, storer = 0;; turn ^= 1, storer = (storer + 1) & 7, ++n_done) {
-        const int lo = tau_lo(it), hi = tau_hi(it), kind = it.kind;
+        const int lo = it.lo, hi = it.hi, kind = kind_of(it);
         const bool full = lo == 0 && hi == 64, valid = tau >= lo && tau < hi;
-        const int64_t plane_tile = (int64_t)it.head * a.table.pool_pages + it.t.page;
+        const int64_t plane_tile = (int64_t)head_of(it) * a.table.pool_pages + it.page;
         uint8_t *gcodes = a.codes[kind] + plane_tile * PQL_CODE_BYTES;
         uint16_t *gradii = a.radii[kind] + plane_tile * kRadiiHalves;
         uint32_t *img = sImg[turn];
-        if (tid == 0) sItem[n_done] = ChunkItem{(int32_t)it.t.page, (int32_t)it.t.row0, (int32_t)it.t.token0, 2 * it.head + kind};
+        if (tid == 0) sItem[n_done] = ChunkItem{it.page, it.row0, it.token0, 2 * head_of(it) + kind};
         if (!full) { /* the tile's present contents */
             const uint32_t *gc = reinterpret_cast<const uint32_t *>(gcodes);
             const uint32_t *gr = reinterpret_cast<const uint32_t *>(gradii);
@@ -532,10 +588,12 @@ __global__ __launch_bounds__(512) void pq_append_chunk_kernel(AppendPagedArgs a,
             __syncthreads();
         }
         if (Op::half) th.radius_scale = base_scale * sUnscale[turn][tau];
-        auto mark = [&](bool doubt) {
-            const uint64_t m = __ballot(doubt && valid);
-            const uint32_t bits = (uint32_t)m | (uint32_t)(m >> 32); /* both halves of the wavefront have the same vectors */
-            if (bits && lane == 0) atomicOr(&sDoubt[n_done][v], bits);
+        auto mark = [&](bool doubt) { /* once per vector, whichever of its codes it is */
+            if (!doubt || !valid) return;
+            const uint32_t bit = 1u << j;
+            if (atomicOr(&sDoubt[n_done][v], bit) & bit) return;
+            const int at = atomicAdd(&sCount, 1);
+            if (at < kListed) sList[at] = (uint32_t)n_done << 6 | (uint32_t)tau;
         };
         if (32 * v < hi && 32 * v + 32 > lo) {
             f32x16 acc = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
@@ -551,7 +609,7 @@ __global__ __launch_bounds__(512) void pq_append_chunk_kernel(AppendPagedArgs a,
                         if (x + term <= Op::top) acc = multiply<PQ_F32, NTERMS>(sa[ks][term], xb[x], acc);
             }
             bool doubt;
-            const BlockCodes bc = quant_block_checked<GENERAL>(acc, th, doubt_of(sNorm2[turn][tau]), w, sPseudo, doubt);
+            const BlockCodes bc = quant_block_checked<GENERAL>(acc, th, doubt_of(sNorm2[turn][tau], levels), levels, sPseudo, doubt);
             mark(doubt);
             if (kind == PQ_KEY) {
                 if (full) leave_block<PQ_KEY, DEEP>(img, tau, 4 * H + rt, bc);
@@ -562,14 +620,18 @@ __global__ __launch_bounds__(512) void pq_append_chunk_kernel(AppendPagedArgs a,
             }
             if (DEEP) sQ4[turn][v][rt][lane] = bc.q4;
         }
-        const bool more = next.index < item_end;
+        const bool more = next.some;
         Item after = next;
         if (more) {
-            leave_row(turn ^ 1, next.kind);
-            after = find(next.index + 1, next);
-            if (after.index < item_end) load_row(after);
+            leave_row(turn ^ 1, kind_of(next));
+            after = following(next);
+            if (after.some) load_row(after);
         }
         __syncthreads();
+        if (more && needs_turn(after)) { /* the rows of the tile before have been turned */
+            load_turn(after);
+            __syncthreads();
+        }
         if (DEEP && rt == 3 && 32 * v < hi && 32 * v + 32 > lo) {
             float q4[4];
 #pragma unroll
@@ -581,10 +643,10 @@ __global__ __launch_bounds__(512) void pq_append_chunk_kernel(AppendPagedArgs a,
             const uint32_t word = H == 0 ? polar_upper_join(mine, far, th.radius_scale, ut) : polar_upper_join(far, mine, th.radius_scale, ut);
             const float err = kDoubt * __builtin_amdgcn_sqrtf(sNorm2[turn][tau]);
             const PqExact &E = *a.exact;
-            mark(upper_in_doubt(q4[0], q4[1], ut.tan2[0], E.up_doubt[0], (1 << ut.b5) - 1, err) ||
-                 upper_in_doubt(q4[2], q4[3], ut.tan2[0], E.up_doubt[0], (1 << ut.b5) - 1, err) ||
-                 upper_in_doubt(q4[0] + q4[1], q4[2] + q4[3], ut.tan2[1], E.up_doubt[1], (1 << ut.b6) - 1, err) ||
-                 upper_in_doubt(H == 0 ? mine.q6 : far.q6, H == 0 ? far.q6 : mine.q6, ut.tan2[2], E.up_doubt[2], (1 << ut.b7) - 1, err));
+            mark(upper_in_doubt(q4[0], q4[1], ut.tan2[0], E.doubt[3], (1 << ut.b5) - 1, err) ||
+                 upper_in_doubt(q4[2], q4[3], ut.tan2[0], E.doubt[3], (1 << ut.b5) - 1, err) ||
+                 upper_in_doubt(q4[0] + q4[1], q4[2] + q4[3], ut.tan2[1], E.doubt[4], (1 << ut.b6) - 1, err) ||
+                 upper_in_doubt(H == 0 ? mine.q6 : far.q6, H == 0 ? far.q6 : mine.q6, ut.tan2[2], E.doubt[5], (1 << ut.b7) - 1, err));
             if (H == 0 && valid) {
                 if (full) reinterpret_cast<uint32_t *>(gradii)[tau] = word;
                 else img[PQL_CODE_BYTES / 4 + tau] = word;
@@ -609,33 +671,36 @@ __global__ __launch_bounds__(512) void pq_append_chunk_kernel(AppendPagedArgs a,
     }
     ++n_done;
 
-    /* ---- the marked vectors in 64 bits: listed 256 at a time, four per turn ---- */
+    /* ---- the vectors in doubt in 64 bits, four per turn.  More than the list holds: lists are made from the marks, 256 vectors at a time. ---- */
     __syncthreads(); /* the workgroup's stores of whole tiles come before its updates of single fields */
-    for (int skip = 0;; skip += 256) {
-        if (wave == 0) {
-            int rank = 0; /* of the first marked vector of the 64 tiles */
-            for (int base = 0; base < n_done; base += 64) {
-                const int i = base + lane;
-                uint64_t m = i < n_done ? (uint64_t)sDoubt[i][1] << 32 | sDoubt[i][0] : 0ull;
-                int incl = __popcll(m);
+    const int in_doubt = sCount;
+    for (int skip = 0; skip < in_doubt; skip += kListed) {
+        if (in_doubt > kListed) {
+            __syncthreads();
+            if (wave == 0) {
+                int rank = 0; /* of the first marked vector of the 64 tiles */
+                for (int base = 0; base < n_done; base += 64) {
+                    const int i = base + lane;
+                    uint64_t m = i < n_done ? (uint64_t)sDoubt[i][1] << 32 | sDoubt[i][0] : 0ull;
+                    int incl = __popcll(m);
 #pragma unroll
-                for (int d = 1; d < 64; d <<= 1) {
-                    const int up = __shfl_up(incl, d);
-                    if (lane >= d) incl += up;
+                    for (int d = 1; d < 64; d <<= 1) {
+                        const int up = __shfl_up(incl, d);
+                        if (lane >= d) incl += up;
+                    }
+                    for (int at = rank + incl - __popcll(m) - skip; m; m &= m - 1, ++at)
+                        if (at >= 0 && at < kListed) sList[at] = (uint32_t)i << 6 | (uint32_t)__builtin_ctzll(m);
+                    rank += __shfl(incl, 63);
                 }
-                for (int at = rank + incl - __popcll(m) - skip; m; m &= m - 1, ++at)
-                    if (at >= 0 && at < 256) sList[at] = (uint32_t)i << 6 | (uint32_t)__builtin_ctzll(m);
-                rank += __shfl(incl, 63);
             }
-            if (lane == 0) sCount = rank - skip;
+            __syncthreads();
         }
-        __syncthreads();
-        const int count = sCount;
-        if (count <= 0) break;
-        const int n = min(count, 256), r = wave >> 1;
+        const int n = min(in_doubt - skip, kListed), r = wave >> 1;
         for (int k = 0; k < n; k += 4) {
             ExactSlice s;
             s.load(a.exact->S, tid);
+            ExactBounds bounds;
+            bounds.load(*a.exact, *a.consts);
             const uint32_t entry = __builtin_amdgcn_readfirstlane(sList[min(k + r, n - 1)]);
             const ChunkItem ci = sItem[entry >> 6];
             const int slot = (int)(entry & 63u), kind = ci.head_kind & 1, head = ci.head_kind >> 1;
@@ -648,8 +713,8 @@ __global__ __launch_bounds__(512) void pq_append_chunk_kernel(AppendPagedArgs a,
             if ((wave & 1) == 0 && k + r < n) {
                 const double ya = rotated_exact(lds.exact, r, 2 * lane), yb = rotated_exact(lds.exact, r, 2 * lane + 1);
                 const int64_t tile = (int64_t)head * a.table.pool_pages + ci.page;
-                if (kind == PQ_KEY) write_exact<PQ_KEY>(a, ya, yb, tile, slot, lane);
-                else write_exact<PQ_VALUE>(a, ya, yb, tile, slot, lane);
+                if (kind == PQ_KEY) write_exact<PQ_KEY>(a, bounds, ya, yb, tile, slot, lane);
+                else write_exact<PQ_VALUE>(a, bounds, ya, yb, tile, slot, lane);
             }
             __syncthreads();
         }
@@ -663,7 +728,8 @@ void launch_chunks(const pq_ctx *ctx, const PqDeviceState *ds, const AppendPaged
     int64_t blocks = n_items < 256 ? n_items : 256; /* one workgroup per CU */
     if (n_items > blocks * kChunkItems) blocks = (n_items + kChunkItems - 1) / kChunkItems;
     auto launch = [&](auto kernel) {
-        hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(512), 0, s, a, reinterpret_cast<const uint4 *>(ds->S_bf16x3), n_items);
+        const uint16_t *terms = ctx->unit_entries || ctx->mixing ? ds->S_f16x2 : ds->S_bf16x3;
+        hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(512), 0, s, a, reinterpret_cast<const uint4 *>(terms), n_items);
     };
     auto with = [&](auto general, auto deep) {
         constexpr bool G = decltype(general)::value, D = decltype(deep)::value;
@@ -693,7 +759,7 @@ extern "C" pq_status pq_append_paged(const pq_ctx *ctx, const void *xk, const vo
     if (xt != PQ_F32 && xt != PQ_BF16) return PQ_EINVAL;
     if (n_rows < 0 || n_seq < 0 || n_heads <= 0 || pool_tokens <= 0 || (pool_tokens & 63) || ld_pages <= 0) return PQ_EINVAL;
     if (ld_token < 0 || ld_head < 0) return PQ_EINVAL;
-    if (n_rows > 0x7FFFFFFF / 2 / n_heads || pool_tokens / 64 > 0x7FFFFFFF) return PQ_EUNSUPPORTED;
+    if (n_rows > 0x7FFFFFFF / 2 / n_heads || n_seq > (1 << 29) || pool_tokens / 64 > 0x7FFFFFFF) return PQ_EUNSUPPORTED;
     const pq_status rs = pq_check_rotary(rotary);
     if (rs != PQ_OK) return rs;
     const int64_t elems16 = xt == PQ_BF16 ? 8 : 4;
