@@ -1452,11 +1452,16 @@ __global__ __launch_bounds__(512) void pq_rotate_q_kernel(RotateArgs a, PlanArgs
 
 /* First launch of attention with prefixes: as above, and one more workgroup builds the plan of the groups' row blocks */
 template <bool ROT>
-__global__ __launch_bounds__(512) void pq_rotate_q_prefix_kernel(RotateArgs a, PlanArgs p, PlanArgs pre, int rows, int row_blocks)
+__global__ __launch_bounds__(512) void pq_rotate_q_prefix_kernel(RotateArgs a, PlanArgs p, PlanArgs pre, BlockRows *blocks, int rows, int row_blocks)
 {
     if ((int)blockIdx.x < row_blocks) rotate_query_rows<ROT>(a, kRotateRows * (int)blockIdx.x, rows);
     else if ((int)blockIdx.x == row_blocks) build_plan(p);
-    else build_plan(pre, [&](int i) { return row_block(a.groups, i, p.B, a.M * (a.Hq / p.Hkv), kPrefixRows).tiles; });
+    else
+        build_plan(pre, [&](int i) {
+            const BlockRows r = row_block(a.groups, i, p.B, a.M * (a.Hq / p.Hkv), kPrefixRows);
+            blocks[i] = r;
+            return (r.tokens + 63) >> 6;
+        });
 }
 
 /* First launch of a whole decode step: the first workgroup builds the work plan (a chain of loads and scans, the
@@ -1961,7 +1966,7 @@ struct StepPrefix {
 /* Row blocks, pieces and workspace of the prefix's part, behind `before` bytes: plan | (m, l) | o' */
 struct PrefixPlan {
     int n_blocks, slots;
-    size_t off_plan, off_ml, off_o, total;
+    size_t off_plan, off_blocks, off_ml, off_o, total;
 };
 
 PrefixPlan make_prefix_plan(int B, int M, int Hq, int Hkv, int n_groups, int64_t max_prefix, size_t before)
@@ -1973,7 +1978,8 @@ PrefixPlan make_prefix_plan(int B, int M, int Hq, int Hkv, int n_groups, int64_t
     p.slots = (int)(most < 256 ? (most < 1 ? 1 : most) : 256); /* one workgroup per CU */
     const size_t pieces = (size_t)p.slots + (size_t)p.n_blocks * Hkv;
     p.off_plan = (before + 255) & ~(size_t)255;
-    p.off_ml = (p.off_plan + (kPlanHeader + (size_t)p.n_blocks + 1 + 2 * (size_t)p.n_blocks * Hkv) * sizeof(int32_t) + 255) & ~(size_t)255;
+    p.off_blocks = (p.off_plan + (kPlanHeader + (size_t)p.n_blocks + 1 + 2 * (size_t)p.n_blocks * Hkv) * sizeof(int32_t) + 255) & ~(size_t)255;
+    p.off_ml = (p.off_blocks + (size_t)p.n_blocks * sizeof(BlockRows) + 255) & ~(size_t)255;
     p.off_o = (p.off_ml + pieces * kPrefixRows * 2 * sizeof(float) + 255) & ~(size_t)255;
     p.total = p.off_o + pieces * kPrefixRows * PQ_D * sizeof(float);
     return p;
@@ -2100,6 +2106,7 @@ pq_status attention_launches(const pq_ctx *ctx, const StepAppend *app, const Ste
                   pq_rotary_args(paged ? paged->rotary : nullptr), paged ? paged->positions : nullptr, ctx_len,
                   pre ? PrefixGroups{pre->group_start, pre->len, pre->n_groups, pre->max_len} : PrefixGroups{}, M, Hq};
     int32_t *pre_plan = reinterpret_cast<int32_t *>(ws + pp.off_plan);
+    BlockRows *pre_blocks = reinterpret_cast<BlockRows *>(ws + pp.off_blocks);
     if (app) {
         AppendArgs ak{app->xk, k_codes, k_radii, pool_tokens / 64, pool_tokens, app->dst_token, Hkv, ds->S_f32, ds->consts, ctx->hadamard};
         AppendArgs av{app->xv, v_codes, v_radii, pool_tokens / 64, pool_tokens, app->dst_token, Hkv, ds->S_f32, ds->consts, ctx->hadamard};
@@ -2123,7 +2130,7 @@ pq_status attention_launches(const pq_ctx *ctx, const StepAppend *app, const Ste
         else hipLaunchKernelGGL(pq_rotate_window_kernel<1>, grid, blk, 0, s, ra, pa, rows, row_blocks, wa, (int)wblocks);
     } else if (pre) {
         const PlanArgs pb{nullptr, nullptr, pp.n_blocks, Hkv, 0, 0, pp.slots, pre_plan};
-        auto rotate = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((unsigned)row_blocks + 2u), dim3(512), 0, s, ra, pa, pb, rows, row_blocks); };
+        auto rotate = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((unsigned)row_blocks + 2u), dim3(512), 0, s, ra, pa, pb, pre_blocks, rows, row_blocks); };
         if (ra.rot.cs) rotate(pq_rotate_q_prefix_kernel<true>);
         else rotate(pq_rotate_q_prefix_kernel<false>);
     } else {
@@ -2154,11 +2161,11 @@ pq_status attention_launches(const pq_ctx *ctx, const StepAppend *app, const Ste
     else partial(std::false_type{});
     if (pre) {
         const PrefixArgs xa{qrot, k_codes, v_codes, k_radii, v_radii, ctx->upper_bits[0], ctx->upper_bits[1], ctx->upper_bits[2],
-                            PagedTable{pre->pages, pre->ld_pages, pool_tokens / 64}, ra.groups, B, Hq, Hkv, M, pre_plan, pp.n_blocks,
+                            PagedTable{pre->pages, pre->ld_pages, pool_tokens / 64}, ra.groups, B, Hq, Hkv, M, pre_plan, pre_blocks, pp.n_blocks,
                             reinterpret_cast<float *>(ws + pp.off_ml), reinterpret_cast<float *>(ws + pp.off_o), ds->consts};
         auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((unsigned)pp.slots), dim3(kPrefixThreads), 0, s, xa); };
-        if (ctx->depth == 7) launch(pq_attn_prefix_kernel<4, true>);
-        else launch(pq_attn_prefix_kernel<4, false>);
+        if (ctx->depth == 7) launch(pq_attn_prefix_kernel<true>);
+        else launch(pq_attn_prefix_kernel<false>);
     }
     pq_prof_after(0, s);
 

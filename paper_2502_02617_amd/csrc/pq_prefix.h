@@ -21,6 +21,12 @@ typedef float f16x __attribute__((ext_vector_type(16)));
 
 constexpr int kPrefixThreads = 512, kPrefixRows = 128;
 
+/* A block of query rows, as the launch that builds the plan leaves it for this one: rows first .. first + rows - 1 of the group that begins with
+ * sequence seq0, and the tokens of its prefix. */
+struct BlockRows {
+    int group, first, rows, seq0, tokens;
+};
+
 struct PrefixArgs {
     const uint16_t *qrot; /* [B][M][Hq][128] binary16 */
     const uint8_t *k_codes, *v_codes;
@@ -30,31 +36,24 @@ struct PrefixArgs {
     PrefixGroups groups;
     int B, Hq, Hkv, M;
     const int32_t *plan; /* as the other kernel's, of row blocks instead of sequences */
+    const BlockRows *blocks;
     int n_blocks;        /* row blocks that the plan counts */
     float *ws_ml; /* [piece][ROWS][2] */
     float *ws_o;  /* [piece][ROWS][128] */
     const PqDeviceConsts *consts;
 };
 
-/* Row blocks of `rows` rows, numbered without a running sum: those of group g begin at start[g] * pairs / rows + g, which leaves room
- * for them (pairs = M * G rows per sequence).  Sequences ahead of start[0] and behind start[n] have no prefix. */
-struct RowBlock {
-    int group;     /* -1: none */
-    int first;     /* first row of the group in the block */
-    int rows;      /* of the block */
-    int seq0;      /* first sequence of the group */
-    int tiles;     /* of the prefix */
-};
-
+/* Row blocks of `rows` rows are numbered without a running sum: those of group g begin at start[g] * pairs / rows + g, which leaves room
+ * for them (pairs = M * G rows per sequence); numbers without rows have no tokens.  Sequences ahead of start[0] and behind start[n] have no prefix. */
 __device__ __forceinline__ int64_t first_block(const PrefixGroups &g, int i, int pairs, int rows)
 {
     return (int64_t)max(g.start[i], 0) * pairs / rows + i;
 }
 
 /* thread by thread (no wavefront operation) */
-__device__ __forceinline__ RowBlock row_block(const PrefixGroups &g, int block, int B, int pairs, int rows)
+__device__ __forceinline__ BlockRows row_block(const PrefixGroups &g, int block, int B, int pairs, int rows)
 {
-    RowBlock r{-1, 0, 0, 0, 0};
+    BlockRows r{-1, 0, 0, 0, 0};
     int lo = 0, hi = g.n; /* the last group that begins at or ahead of the block */
     while (lo < hi) {
         const int mid = (lo + hi) >> 1;
@@ -70,7 +69,7 @@ __device__ __forceinline__ RowBlock row_block(const PrefixGroups &g, int block, 
     r.first = (int)first;
     r.rows = (int)min(all - first, (int64_t)rows);
     r.seq0 = s0;
-    r.tiles = (prefix_length(g, i) + 63) >> 6;
+    r.tokens = prefix_length(g, i);
     return r;
 }
 
@@ -81,37 +80,140 @@ __device__ __forceinline__ int query_row(int seq0, int i, int M, int Hq, int G, 
     return ((seq0 + s) * M + m) * Hq + hk * G + (rest - m * G);
 }
 
-/* A tile as it is in memory, codes and radii, to LDS (8 loads in all of the wavefronts that call it). */
+/* A tile as it is in memory, codes and radii behind them. */
 struct RawTile { __attribute__((aligned(16))) uint32_t w[1024]; };
 
-/* ROWS = 32 * ROW_WAVES rows per workgroup; 8 / ROW_WAVES wavefronts share a tile's tokens. */
-template <int ROW_WAVES, bool DEEP>
+/* Place of eight tokens of a coordinate in the values' LDS: neighbouring coordinates are read together, every eighth is written together. */
+__device__ __forceinline__ int value_place(int coordinate, int chunk) { return 8 * coordinate + (chunk ^ (((coordinate >> 1) ^ (coordinate >> 3)) & 7)); }
+
+struct PrefixTables {
+    __attribute__((aligned(16))) uint32_t tq[2048];
+    __attribute__((aligned(16))) float tbf[64][4];
+    __attribute__((aligned(16))) uint32_t tbh[128];
+    float2 up[24];
+};
+
+/* What a wavefront rebuilds of a tile: block `wave` of the keys of all 64 tokens, a token per lane, and half-block n of the values of the two
+ * tokens 16 i + 4 g + e0, + 1 per lane (g, n), i = wave / 2, e0 = 2 (wave % 2).  In three steps, so that other work covers their LDS
+ * reads.  Tokens from nv on become zeros, whatever the page holds there; products are binary16, radius times block table times quarter table, as
+ * the values' of the other kernel. */
+template <bool DEEP>
+struct Rebuild {
+    uint32_t kx0, kx1, vx0, vx1, vb, kr, vr;
+    h2 kq[2], vq[2];   /* radii of the quarters: the key's four, the values' two of each token */
+    uint2 kt[4], vt[4];
+
+    /* the strings' dwords; `raw` as in memory */
+    __device__ __forceinline__ void fetch(const uint32_t *rk, const uint32_t *rv, int wave, int lane)
+    {
+        /* dword d of a key's string lies at base + stride * token bytes: planes of 16, 16, 12 and 2 bytes per token */
+        const int bit = PQL_BLOCK_BITS * wave, d0 = bit >> 5, sh = bit & 31;
+        const char *k = reinterpret_cast<const char *>(rk), *v = reinterpret_cast<const char *>(rv);
+        auto key_dword = [&](int d) {
+            const int base = d < 4 ? PQL_OFF_P0 + 4 * d : (d < 8 ? PQL_OFF_P1 + 4 * (d - 4) : PQL_OFF_P2 + 4 * (d - 8));
+            const int at = d < 11 ? base + (d < 8 ? 16 : 12) * lane : PQL_OFF_KP3 + ((2 * lane) & ~3);
+            const uint32_t x = *reinterpret_cast<const uint32_t *>(k + at);
+            return d < 11 ? x : x >> (16 * (lane & 1)); /* the last half; behind it nothing is looked at */
+        };
+        const uint32_t w0 = key_dword(d0), w1 = key_dword(d0 + 1), w2 = key_dword(min(d0 + 2, 11));
+        kx0 = __builtin_amdgcn_alignbit(w1, w0, sh);
+        kx1 = __builtin_amdgcn_alignbit(w2, w1, sh);
+        kr = DEEP ? rk[kKeyRadii + lane] : reinterpret_cast<const uint16_t *>(rk + kKeyRadii)[8 * lane + wave];
+        /* slots s, s + 1 = 4 i + e0: bits [20 s, 20 s + 40) of the string, [6 s, 6 s + 12) of the block indices */
+        const int s = 4 * (wave >> 1) + 2 * (wave & 1), e0 = (20 * s) >> 5, vsh = (20 * s) & 31;
+        auto value_dword = [&](int d) {
+            const int at = d < 8 ? (d < 4 ? PQL_OFF_P0 + 4 * d : PQL_OFF_P1 + 4 * (d - 4)) + 16 * lane : PQL_OFF_P2 + 4 * (d - 8) + 8 * lane;
+            return *reinterpret_cast<const uint32_t *>(v + at);
+        };
+        const uint32_t v0 = value_dword(e0), v1 = value_dword(min(e0 + 1, 9)), v2 = value_dword(min(e0 + 2, 9));
+        vx0 = __builtin_amdgcn_alignbit(v1, v0, vsh);
+        vx1 = __builtin_amdgcn_alignbit(v2, v1, vsh);
+        const uint32_t *b = rv + PQL_OFF_VB / 4 + 3 * (lane >> 1);
+        const int b0 = (6 * s) >> 5;
+        vb = __builtin_amdgcn_alignbit(b[min(b0 + 1, 2)], b[b0], (6 * s) & 31);
+        if (!DEEP) vr = *reinterpret_cast<const uint32_t *>(reinterpret_cast<const uint16_t *>(rv + kKeyRadii) + (lane >> 1) * 16 + s);
+    }
+
+    /* the tables' entries */
+    __device__ __forceinline__ void gather(const PrefixArgs &a, const PrefixTables &tab, const uint32_t *rv, int wave, int nv, int lane)
+    {
+        const int n = lane & 15, t0 = 16 * (wave >> 1) + 4 * (lane >> 4) + 2 * (wave & 1);
+        float r = DEEP ? pq_deep_block_radius(kr, a.up_b5, a.up_b6, a.up_b7, tab.up, wave) : pq_half_bits_to_float(kr);
+        if (lane >= nv) r = 0.f;
+        const float4 t43 = *reinterpret_cast<const float4 *>(tab.tbf[(kx1 >> 8) & 63u]);
+        if (DEEP) {
+            float f[2];
+#pragma unroll
+            for (int e = 0; e < 2; ++e) f[e] = pq_deep_block_radius(rv[kKeyRadii + t0 + e], a.up_b5, a.up_b6, a.up_b7, tab.up, n >> 1);
+            vr = __builtin_bit_cast(uint32_t, h2{(_Float16)f[0], (_Float16)f[1]});
+        }
+        if (t0 >= nv) vr = 0u;
+        else if (t0 + 1 >= nv) vr &= 0xFFFFu;
+        const uint32_t h0 = tab.tbh[2 * (vb & 63u) + (n & 1)], h1 = tab.tbh[2 * ((vb >> 6) & 63u) + (n & 1)];
+        const uint32_t K[4] = {kx0 & 1023u, (kx0 >> 10) & 1023u, (kx0 >> 20) & 1023u, __builtin_amdgcn_alignbit(kx1, kx0, 30) & 1023u};
+        const uint32_t V[4] = {vx0 & 1023u, (vx0 >> 10) & 1023u, (vx0 >> 20) & 1023u, __builtin_amdgcn_alignbit(vx1, vx0, 30) & 1023u};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            kt[j] = *reinterpret_cast<const uint2 *>(tab.tq + 2 * K[j]);
+            vt[j] = *reinterpret_cast<const uint2 *>(tab.tq + 2 * V[j]);
+        }
+        kq[0] = h2{(_Float16)(r * t43.x), (_Float16)(r * t43.y)};
+        kq[1] = h2{(_Float16)(r * t43.z), (_Float16)(r * t43.w)};
+        const h2 two = as_h2(vr);
+        vq[0] = bcast_lo(two) * as_h2(h0);
+        vq[1] = bcast_hi(two) * as_h2(h1);
+    }
+
+    /* their products, to LDS; token 4 g + e of sixteen goes to place 8 (g & 1) + 4 (g >> 1) + e, the order of the weights in the lanes */
+    __device__ __forceinline__ void store(uint4 *sK, uint4 *sV, int wave, int lane)
+    {
+        H8 o[2];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const h2 f = (j & 1) ? bcast_hi(kq[j >> 1]) : bcast_lo(kq[j >> 1]);
+            o[j >> 1].p[2 * (j & 1)] = f * as_h2(kt[j].x);
+            o[j >> 1].p[2 * (j & 1) + 1] = f * as_h2(kt[j].y);
+        }
+        sK[16 * lane + ((2 * wave) ^ (lane & 15))] = o[0].q;
+        sK[16 * lane + ((2 * wave + 1) ^ (lane & 15))] = o[1].q;
+        const int g = lane >> 4, n = lane & 15, chunk = 2 * (wave >> 1) + (g & 1), part = 2 * (g >> 1) + (wave & 1);
+#pragma unroll
+        for (int c = 0; c < 4; ++c) { /* coordinates 2 c, 2 c + 1 of the half-block: quarter c / 2, product c % 2 */
+            const h2 f0 = (c & 2) ? bcast_hi(vq[0]) : bcast_lo(vq[0]), f1 = (c & 2) ? bcast_hi(vq[1]) : bcast_lo(vq[1]);
+            const uint2 t0 = vt[c >> 1], t1 = vt[2 + (c >> 1)];
+            const uint32_t x = __builtin_bit_cast(uint32_t, f0 * as_h2((c & 1) ? t0.y : t0.x)), y = __builtin_bit_cast(uint32_t, f1 * as_h2((c & 1) ? t1.y : t1.x));
+            reinterpret_cast<uint32_t *>(sV)[4 * value_place(8 * n + 2 * c, chunk) + part] = __builtin_amdgcn_perm(y, x, 0x05040100u);
+            reinterpret_cast<uint32_t *>(sV)[4 * value_place(8 * n + 2 * c + 1, chunk) + part] = __builtin_amdgcn_perm(y, x, 0x07060302u);
+        }
+    }
+};
+
+/* kPrefixRows rows per workgroup, 32 per wavefront; two wavefronts share rows and have half of a tile's tokens each.  While a tile is
+ * multiplied the next one is rebuilt into the other half of LDS, and the one after that is on its way there: one barrier per tile.  What
+ * bounds it is the chain of a wavefront's steps, two wavefronts per SIMD: so all requests to LDS stand ahead of the work that covers them. */
+template <bool DEEP>
 __global__ __launch_bounds__(kPrefixThreads, 1) void pq_attn_prefix_kernel(PrefixArgs a)
 {
-    constexpr int kRows = 32 * ROW_WAVES, kSlices = 8 / ROW_WAVES; /* token slices of 32 */
-    static_assert(ROW_WAVES == 4 && kSlices == 2 && kRows == kPrefixRows, "a tile is two slices of 32 tokens");
-    __shared__ __attribute__((aligned(16))) uint32_t sTQ[2048];
-    __shared__ __attribute__((aligned(16))) float sTBF[64][4];
-    __shared__ __attribute__((aligned(16))) uint32_t sTBH[128];
-    __shared__ float2 sUp[24];
-    __shared__ RawTile sRaw[2][2]; /* [buffer][keys, values] */
-    __shared__ __attribute__((aligned(16))) uint4 sK[64 * 16];  /* [token][chunk of eight coordinates ^ token & 15] */
-    __shared__ __attribute__((aligned(16))) uint4 sV[128 * 8];  /* [coordinate][chunk of eight tokens ^ value_swizzle] */
-    __shared__ __attribute__((aligned(16))) uint16_t sVrad[DEEP ? 512 : 8];
-    __shared__ float sM[ROW_WAVES][32][2];
+    static_assert(kPrefixRows == 128 && kPrefixThreads == 512, "four row groups, two slices of 32 tokens");
+    __shared__ PrefixTables tab;
+    __shared__ RawTile sRaw[2][2];                                 /* [buffer][keys, values] */
+    __shared__ __attribute__((aligned(16))) uint4 sK[2][64 * 16];  /* [token][chunk of eight coordinates ^ token & 15] */
+    __shared__ __attribute__((aligned(16))) uint4 sV[2][128 * 8];  /* value_place */
+    __shared__ float sM[4][32][2];
 
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int total = a.plan[0], working = a.plan[1];
     const int w = (int)blockIdx.x;
+    const int total = a.plan[0], working = a.plan[1];
     {
         const uint32_t *src = a.consts->attn_tab;
-        reinterpret_cast<uint4 *>(sTQ)[tid] = reinterpret_cast<const uint4 *>(src + PQ_TAB_TQ)[tid];
-        if (tid < 256) (&sTBF[0][0])[tid] = __uint_as_float(src[PQ_TAB_TBF + tid]);
-        if (tid < 128) sTBH[tid] = src[PQ_TAB_TBH + tid];
-        if (tid < 48) reinterpret_cast<uint32_t *>(sUp)[tid] = src[PQ_TAB_UP + tid];
+        const uint4 t = reinterpret_cast<const uint4 *>(src + PQ_TAB_TQ)[tid];
+        const uint32_t f = src[PQ_TAB_TBF + (tid & 255)], h = src[PQ_TAB_TBH + (tid & 127)], u = src[PQ_TAB_UP + min(tid, 47)];
+        reinterpret_cast<uint4 *>(tab.tq)[tid] = t;
+        if (tid < 256) (&tab.tbf[0][0])[tid] = __uint_as_float(f);
+        if (tid < 128) tab.tbh[tid] = h;
+        if (tid < 48) reinterpret_cast<uint32_t *>(tab.up)[tid] = u;
     }
-    __syncthreads();
     if (w >= working) return;
     const int base = total / working, rem = total - base * working;
     int gpos = w * base + min(w, rem);
@@ -120,30 +222,50 @@ __global__ __launch_bounds__(kPrefixThreads, 1) void pq_attn_prefix_kernel(Prefi
     int blk = paged_find(a.n_blocks, gpos, lane, [&](int i) { return (int64_t)a.plan[kPlanHeader + i] * a.Hkv; });
     blk = min(max(blk, 0), a.n_blocks - 1);
     int before = a.plan[kPlanHeader + blk], block_tiles = a.plan[kPlanHeader + blk + 1] - before;
-    if (block_tiles <= 0) return;
+    if (block_tiles <= 0) return; /* cannot happen with a consistent plan */
     int hk, tile_lo;
     {
         const int r = gpos - before * a.Hkv;
         hk = min(r / block_tiles, a.Hkv - 1);
         tile_lo = r - hk * block_tiles;
     }
-    const int G = a.Hq / a.Hkv, pairs = a.M * G;
+    const int G = a.Hq / a.Hkv;
     constexpr int kRadiiHalves = DEEP ? PQ_DEEP_RADII_HALVES : PQL_RADII;
-    const int rg = wave / kSlices, slice = wave % kSlices, H = lane >> 5, r32 = lane & 31;
-    auto value_swizzle = [](int c) { return ((c >> 1) ^ (c >> 3)) & 7; };
+    const int rg = (wave >> 1) & 3, slice = wave & 1, H = lane >> 5, r32 = lane & 31;
 
     for (;;) { /* one piece per round */
-        const RowBlock rb = row_block(a.groups, blk, a.B, pairs, kRows);
-        const int n_tok = rb.group >= 0 ? prefix_length(a.groups, rb.group) : 0;
-        const int tile_hi = min((n_tok + 63) >> 6, tile_lo + (gend - gpos));
+        const BlockRows rb = a.blocks[blk];
+        const int tile_hi = min((rb.tokens + 63) >> 6, tile_lo + (gend - gpos));
         const int piece_tiles = tile_hi - tile_lo;
         if (piece_tiles <= 0) return; /* cannot happen with a consistent plan */
         const int64_t piece = (int64_t)w + (int64_t)blk * a.Hkv + hk;
-        const int row = rb.first + 32 * rg + r32; /* of the group */
+        /* keys by wavefront 0, values by wavefront 1 (wavefronts of two SIMDs); a tile without a page is passed over */
+        int page_base = tile_lo; /* the table's entries of 64 tiles lie in a register, one per lane */
+        int32_t page_reg = 0;
+        auto fetch_pages = [&](int t) {
+            page_base = t;
+            page_reg = a.table.pages[(int64_t)rb.group * a.table.ld_pages + min(t + lane, tile_hi - 1)];
+        };
+        auto page_of = [&](int t) {
+            if (t >= tile_hi) return -1;
+            if (t - page_base >= 64) fetch_pages(t);
+            const int p = __builtin_amdgcn_readlane(page_reg, t - page_base);
+            return p >= 0 && p < a.table.pool_pages ? p : -1;
+        };
+        auto request = [&](int buffer, int page) {
+            if (wave > 1 || page < 0) return;
+            const int64_t at = (int64_t)hk * a.table.pool_pages + page;
+            const uint8_t *codes = (wave ? a.v_codes : a.k_codes) + at * PQL_CODE_BYTES;
+            const uint16_t *radii = (wave ? a.v_radii : a.k_radii) + at * kRadiiHalves;
+            request_k_tile<DEEP>(sRaw[buffer][wave].w, stream_descriptor(codes, PQL_CODE_BYTES), stream_descriptor(radii, kRadiiHalves * 2), 0, lane);
+        };
+        fetch_pages(tile_lo);
+        int page = page_of(tile_lo), page1 = page_of(tile_lo + 1); /* of the tile that is multiplied, and the next */
+        request(tile_lo & 1, page);
         const bool real = 32 * rg + r32 < rb.rows;
         h8 q[8];
         {
-            const int64_t at = (int64_t)query_row(rb.seq0, real ? row : rb.first, a.M, a.Hq, G, hk) * PQ_D;
+            const int64_t at = (int64_t)query_row(rb.seq0, rb.first + (real ? 32 * rg + r32 : 0), a.M, a.Hq, G, hk) * PQ_D;
             const uint4 *qr = reinterpret_cast<const uint4 *>(a.qrot + at) + H;
 #pragma unroll
             for (int ks = 0; ks < 8; ++ks) {
@@ -160,136 +282,55 @@ __global__ __launch_bounds__(kPrefixThreads, 1) void pq_attn_prefix_kernel(Prefi
             for (int e = 0; e < 16; ++e) acc[d][e] = 0.f;
         float m_ref = 0.f, l_run = 0.f;
         bool have_ref = false;
-
-        /* keys by wavefront 0, values by wavefront 1; false: the tile has no page and is passed over */
-        auto page_of = [&](int t) { return paged_page(a.table, rb.group, (int64_t)t * 64); };
-        auto request = [&](int buffer, int64_t page) {
-            if (wave > 1 || page < 0) return;
-            const int64_t at = (int64_t)hk * a.table.pool_pages + page;
-            const uint8_t *codes = (wave ? a.v_codes : a.k_codes) + at * PQL_CODE_BYTES;
-            const uint16_t *radii = (wave ? a.v_radii : a.k_radii) + at * kRadiiHalves;
-            request_k_tile<DEEP>(sRaw[buffer][wave].w, stream_descriptor(codes, PQL_CODE_BYTES), stream_descriptor(radii, kRadiiHalves * 2), 0, lane);
-        };
-        int64_t page = page_of(tile_lo);
-        request(0, page);
+        /* tokens of tile t that are looked at: a tile without a page has none */
+        auto tokens_of = [&](int t, int p) { return p < 0 ? 0 : min(rb.tokens - 64 * t, 64); };
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        __syncthreads(); /* the tables and the first raw tile are there */
+        request((tile_lo + 1) & 1, page1);
+        {
+            Rebuild<DEEP> r;
+            r.fetch(sRaw[tile_lo & 1][0].w, sRaw[tile_lo & 1][1].w, wave, lane);
+            r.gather(a, tab, sRaw[tile_lo & 1][1].w, wave, tokens_of(tile_lo, page), lane);
+            r.store(sK[tile_lo & 1], sV[tile_lo & 1], wave, lane);
+        }
         for (int tile = tile_lo; tile < tile_hi; ++tile) {
-            const int buffer = (tile - tile_lo) & 1;
-            const int64_t next_page = tile + 1 < tile_hi ? page_of(tile + 1) : -1;
+            const int cur = tile & 1, nxt = cur ^ 1;
+            const int page2 = page_of(tile + 2);
             asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-            __syncthreads(); /* the raw tile has arrived, and nobody reads the tile before it any more */
-            request(buffer ^ 1, next_page);
-            const bool missing = page < 0;
-            page = next_page;
-            if (missing) continue;
-            const int nv = min(n_tok - 64 * tile, 64); /* tokens of the tile */
-            const uint32_t *rk = sRaw[buffer][0].w, *rv = sRaw[buffer][1].w;
-            if (DEEP && wave < 4) { /* radii of the blocks, in the order of a depth-4 tile */
-                if (wave == 0) {
-                    float r[8];
-                    pq_deep_block_radii(rv[kKeyRadii + lane], a.up_b5, a.up_b6, a.up_b7, sUp, r);
-                    const int i = lane >> 4, g = (lane >> 2) & 3, e = lane & 3;
+            __syncthreads(); /* this tile is rebuilt, the next raw one has arrived, and nobody reads the tile before this one any more */
+            request(cur, page2);
+            int l = lane; /* addresses are formed where they are used: kept over the tile loop they would be spilled */
+            asm volatile("" : "+v"(l));
+            const int nv = tokens_of(tile, page), nv1 = tokens_of(tile + 1, page1);
+            const int lH = l >> 5, lr = l & 31, tok = 32 * slice + lr;
+            Rebuild<DEEP> r;
+            r.fetch(sRaw[nxt][0].w, sRaw[nxt][1].w, wave, l);
+            H8 ko[8];
 #pragma unroll
-                    for (int b = 0; b < 8; ++b) sVrad[(8 * g + b) * 16 + 4 * i + e] = __builtin_bit_cast(uint16_t, (_Float16)r[b]);
-                }
-            }
-            if (DEEP) __syncthreads();
-            if (wave >= 4) { /* keys: two blocks per wavefront, a token per lane */
-                const int tau = lane;
-                float r8[8];
-                if (DEEP) pq_deep_block_radii(rk[kKeyRadii + tau], a.up_b5, a.up_b6, a.up_b7, sUp, r8);
-#pragma unroll
-                for (int k = 0; k < 2; ++k) {
-                    const int b = 2 * (wave - 4) + k;
-                    auto dword = [&](int d) -> uint32_t {
-                        if (d < 4) return rk[4 * tau + d];
-                        if (d < 8) return rk[256 + 4 * tau + d - 4];
-                        if (d < 11) return rk[512 + 3 * tau + d - 8];
-                        return reinterpret_cast<const uint16_t *>(rk)[PQL_OFF_KP3 / 2 + tau];
-                    };
-                    const int bit = PQL_BLOCK_BITS * b, d0 = bit >> 5, sh = bit & 31;
-                    const uint32_t w0 = dword(d0), w1 = dword(d0 + 1), w2 = d0 + 2 < 12 ? dword(d0 + 2) : 0u;
-                    const uint32_t x[2] = {__builtin_amdgcn_alignbit(w1, w0, sh), __builtin_amdgcn_alignbit(w2, w1, sh)};
-                    float r;
-                    if (DEEP) {
-                        r = r8[0];
-#pragma unroll
-                        for (int e = 1; e < 8; ++e) r = b == e ? r8[e] : r;
-                    } else {
-                        r = pq_half_bits_to_float(reinterpret_cast<const uint16_t *>(rk + kKeyRadii)[8 * tau + b]);
-                    }
-                    if (tau >= nv) r = 0.f;
-                    const float4 t43 = *reinterpret_cast<const float4 *>(sTBF[(x[1] >> 8) & 63u]);
-                    const float rq[4] = {r * t43.x, r * t43.y, r * t43.z, r * t43.w};
-                    const uint32_t Q[4] = {x[0] & 1023u, (x[0] >> 10) & 1023u, (x[0] >> 20) & 1023u, __builtin_amdgcn_alignbit(x[1], x[0], 30) & 1023u};
-                    H8 o[2];
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        const uint2 t = *reinterpret_cast<const uint2 *>(sTQ + 2 * Q[j]);
-#pragma unroll
-                        for (int c = 0; c < 2; ++c) {
-                            const h2 two = as_h2(c ? t.y : t.x);
-                            o[j >> 1].p[2 * (j & 1) + c] = h2{(_Float16)(rq[j] * (float)two.x), (_Float16)(rq[j] * (float)two.y)};
-                        }
-                    }
-                    sK[16 * tau + ((2 * b) ^ (tau & 15))] = o[0].q;
-                    sK[16 * tau + ((2 * b + 1) ^ (tau & 15))] = o[1].q;
-                }
-            } else { /* values: sixteen tokens per wavefront, lane (g, n) four of them of half-block n */
-                const int i = wave, g = lane >> 4, n = lane & 15;
-                auto dword = [&](int d) { return d < 4 ? rv[4 * lane + d] : (d < 8 ? rv[256 + 4 * lane + d - 4] : rv[512 + 2 * lane + d - 8]); };
-                /* slots 4 i .. 4 i + 3: bits [80 i, 80 i + 80) of the string, [24 i, 24 i + 24) of the block indices */
-                const int d0 = (80 * i) >> 5, sh = (80 * i) & 31;
-                const uint32_t w0 = dword(d0), w1 = dword(d0 + 1), w2 = dword(d0 + 2), w3 = d0 + 3 < 10 ? dword(d0 + 3) : 0u;
-                const uint32_t x[3] = {__builtin_amdgcn_alignbit(w1, w0, sh), __builtin_amdgcn_alignbit(w2, w1, sh), __builtin_amdgcn_alignbit(w3, w2, sh)};
-                const uint32_t *vb = rv + PQL_OFF_VB / 4 + 3 * (lane >> 1);
-                const int e0 = (24 * i) >> 5, bs = (24 * i) & 31;
-                const uint32_t bi = __builtin_amdgcn_alignbit(e0 + 1 < 3 ? vb[e0 + 1] : 0u, vb[e0], bs);
-                const uint16_t *rad = DEEP ? sVrad : reinterpret_cast<const uint16_t *>(rv + kKeyRadii);
-                const uint2 r4 = *reinterpret_cast<const uint2 *>(rad + (lane >> 1) * 16 + 4 * i);
-                const uint32_t F[4] = {x[0] & 0xFFFFFu, __builtin_amdgcn_alignbit(x[1], x[0], 20) & 0xFFFFFu, (x[1] >> 8) & 0xFFFFFu,
-                                       __builtin_amdgcn_alignbit(x[2], x[1], 28) & 0xFFFFFu};
-                h2 ve[4][4]; /* [token][pair of coordinates] */
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const h2 two = as_h2((e & 2) ? r4.y : r4.x);
-                    h2 r = (e & 1) ? bcast_hi(two) : bcast_lo(two);
-                    if (16 * i + 4 * g + e >= nv) r = h2{(_Float16)0.f, (_Float16)0.f};
-                    const h2 rq = r * as_h2(sTBH[2 * ((bi >> (6 * e)) & 63u) + (n & 1)]);
-                    const uint2 ta = *reinterpret_cast<const uint2 *>(sTQ + 2 * (F[e] & 1023u));
-                    const uint2 tb = *reinterpret_cast<const uint2 *>(sTQ + 2 * (F[e] >> 10));
-                    ve[e][0] = bcast_lo(rq) * as_h2(ta.x);
-                    ve[e][1] = bcast_lo(rq) * as_h2(ta.y);
-                    ve[e][2] = bcast_hi(rq) * as_h2(tb.x);
-                    ve[e][3] = bcast_hi(rq) * as_h2(tb.y);
-                }
-                /* token 16 i + 4 g + e of a group of sixteen goes to place 8 (g & 1) + 4 (g >> 1) + e of it */
-                const int chunk = 2 * i + (g & 1), part = g >> 1;
-#pragma unroll
-                for (int c = 0; c < 8; ++c) {
-                    const uint32_t sel = (c & 1) ? 0x07060302u : 0x05040100u;
-                    const uint32_t lo = __builtin_amdgcn_perm(__builtin_bit_cast(uint32_t, ve[1][c >> 1]), __builtin_bit_cast(uint32_t, ve[0][c >> 1]), sel);
-                    const uint32_t hi = __builtin_amdgcn_perm(__builtin_bit_cast(uint32_t, ve[3][c >> 1]), __builtin_bit_cast(uint32_t, ve[2][c >> 1]), sel);
-                    const int dim = 8 * n + c;
-                    reinterpret_cast<uint2 *>(sV)[2 * (8 * dim + (chunk ^ value_swizzle(dim))) + part] = make_uint2(lo, hi);
-                }
-            }
-            __syncthreads();
+            for (int ks = 0; ks < 8; ++ks) ko[ks].q = sK[cur][16 * tok + ((2 * ks + lH) ^ (tok & 15))];
+            __builtin_amdgcn_sched_barrier(0);
+            r.gather(a, tab, sRaw[nxt][1].w, wave, nv1, l);
             f16x s;
 #pragma unroll
             for (int e = 0; e < 16; ++e) s[e] = kProbShift - m_ref;
-            const int tok = 32 * slice + r32;
 #pragma unroll
-            for (int ks = 0; ks < 8; ++ks)
-                s = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(h8, sK[16 * tok + ((2 * ks + H) ^ (tok & 15))]), q[ks], s, 0, 0, 0);
+            for (int ks = 0; ks < 8; ++ks) s = __builtin_amdgcn_mfma_f32_32x32x16_f16(ko[ks].v, q[ks], s, 0, 0, 0);
+            __builtin_amdgcn_sched_barrier(0);
+            H8 vo[8];
+#pragma unroll
+            for (int d = 0; d < 4; ++d)
+#pragma unroll
+                for (int k = 0; k < 2; ++k) vo[2 * d + k].q = sV[cur][value_place(32 * d + lr, 2 * (2 * slice + k) + lH)];
             if (nv < 64) {
 #pragma unroll
                 for (int e = 0; e < 16; ++e)
-                    if (32 * slice + 8 * (e >> 2) + 4 * H + (e & 3) >= nv) s[e] = -INFINITY;
+                    if (32 * slice + 8 * (e >> 2) + 4 * lH + (e & 3) >= nv) s[e] = -INFINITY;
             }
             float top = s[0];
 #pragma unroll
             for (int e = 1; e < 16; ++e) top = fmaxf(top, s[e]);
-            if (!have_ref || __ballot(top > kProbShift + kRefSlack) != 0ull) {
+            /* the first tokens that this slice sees set the reference of its rows */
+            if (nv > 32 * slice && (!have_ref || __ballot(top > kProbShift + kRefSlack) != 0ull)) {
                 top = fmaxf(top, __shfl_xor(top, 32));
                 float delta = top == -INFINITY ? 0.f : top - kProbShift;
                 if (have_ref) delta = fmaxf(delta, 0.f);
@@ -304,59 +345,59 @@ __global__ __launch_bounds__(kPrefixThreads, 1) void pq_attn_prefix_kernel(Prefi
             }
             H8 p[2];
 #pragma unroll
-            for (int e = 0; e < 16; ++e) {
-                const float x = __builtin_amdgcn_exp2f(s[e]);
-                l_run += x;
-                p[e >> 3].v[e & 7] = (_Float16)x;
+            for (int e = 0; e < 16; e += 2) {
+                const float x = __builtin_amdgcn_exp2f(s[e]), y = __builtin_amdgcn_exp2f(s[e + 1]);
+                l_run += x + y;
+                p[e >> 3].p[(e & 7) >> 1] = h2{(_Float16)x, (_Float16)y};
             }
 #pragma unroll
-            for (int d = 0; d < 4; ++d)
+            for (int k = 0; k < 2; ++k)
 #pragma unroll
-                for (int k = 0; k < 2; ++k) {
-                    const int dim = 32 * d + r32, chunk = 2 * (2 * slice + k) + H;
-                    acc[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(h8, sV[8 * dim + (chunk ^ value_swizzle(dim))]), p[k].v, acc[d], 0, 0, 0);
-                }
+                for (int d = 0; d < 4; ++d) acc[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vo[2 * d + k].v, p[k].v, acc[d], 0, 0, 0);
+            r.store(sK[nxt], sV[nxt], wave, l);
+            page = page1;
+            page1 = page2;
         }
-        /* ---- the slices' results joined (through the keys' and values' LDS, a quarter of the coordinates at a time), and stored ---- */
+        /* ---- the slices' results joined (through LDS, half of the coordinates at a time), and stored ---- */
         float l = l_run + __shfl_xor(l_run, 32), m = l > 0.f ? m_ref : -INFINITY;
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         __syncthreads();
         if (slice == 1 && H == 0) {
             sM[rg][r32][0] = m;
             sM[rg][r32][1] = l;
         }
-        __syncthreads();
+        float4 *theirs = reinterpret_cast<float4 *>(&sK[0][0]) + rg * 512 + lane; /* eight of 64 lanes each */
+        const int64_t out_row = piece * kPrefixRows + 32 * rg + r32;
         float scale0 = 0.f, scale1 = 0.f;
-        {
-            const float m1 = sM[rg][r32][0], l1 = sM[rg][r32][1];
-            if (slice == 0) {
-                const float mm = fmaxf(m, m1);
-                if (mm != -INFINITY) {
-                    scale0 = __builtin_amdgcn_exp2f(m - mm);
-                    scale1 = __builtin_amdgcn_exp2f(m1 - mm);
-                }
-                l = l * scale0 + l1 * scale1;
-                m = mm;
-            }
-        }
-        float *mine = reinterpret_cast<float *>(sK) + (rg * 64 + lane) * 16;
-        const int64_t out_row = piece * kRows + 32 * rg + r32;
 #pragma unroll
-        for (int d = 0; d < 4; ++d) {
+        for (int half = 0; half < 2; ++half) {
             if (slice == 1) {
 #pragma unroll
-                for (int e = 0; e < 16; ++e) mine[e] = acc[d][e];
+                for (int k = 0; k < 8; ++k) {
+                    const f16x &o = acc[2 * half + (k >> 2)];
+                    theirs[64 * k] = make_float4(o[4 * (k & 3)], o[4 * (k & 3) + 1], o[4 * (k & 3) + 2], o[4 * (k & 3) + 3]);
+                }
             }
             __syncthreads();
-            if (slice == 0 && real) {
+            if (slice == 0) {
+                if (half == 0) {
+                    const float m1 = sM[rg][r32][0], l1 = sM[rg][r32][1], mm = fmaxf(m, m1);
+                    if (mm != -INFINITY) {
+                        scale0 = __builtin_amdgcn_exp2f(m - mm);
+                        scale1 = __builtin_amdgcn_exp2f(m1 - mm);
+                    }
+                    l = l * scale0 + l1 * scale1;
+                    m = mm;
+                }
+                if (real) {
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    float4 o;
-                    o.x = acc[d][4 * j] * scale0 + mine[4 * j] * scale1;
-                    o.y = acc[d][4 * j + 1] * scale0 + mine[4 * j + 1] * scale1;
-                    o.z = acc[d][4 * j + 2] * scale0 + mine[4 * j + 2] * scale1;
-                    o.w = acc[d][4 * j + 3] * scale0 + mine[4 * j + 3] * scale1;
-                    *reinterpret_cast<float4 *>(a.ws_o + out_row * PQ_D + 32 * d + 8 * j + 4 * H) = o;
+                    for (int k = 0; k < 8; ++k) {
+                        const f16x &o = acc[2 * half + (k >> 2)];
+                        const float4 t = theirs[64 * k];
+                        const int j = k & 3;
+                        const float4 sum = make_float4(o[4 * j] * scale0 + t.x * scale1, o[4 * j + 1] * scale0 + t.y * scale1,
+                                                       o[4 * j + 2] * scale0 + t.z * scale1, o[4 * j + 3] * scale0 + t.w * scale1);
+                        *reinterpret_cast<float4 *>(a.ws_o + out_row * PQ_D + 32 * (2 * half + (k >> 2)) + 8 * j + 4 * H) = sum;
+                    }
                 }
             }
             __syncthreads();
