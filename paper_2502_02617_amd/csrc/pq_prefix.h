@@ -97,41 +97,57 @@ struct PrefixTables {
  * tokens 16 i + 4 g + e0, + 1 per lane (g, n), i = wave / 2, e0 = 2 (wave % 2).  In three steps, so that other work covers their LDS
  * reads.  Tokens from nv on become zeros, whatever the page holds there; products are binary16, radius times block table times quarter table, as
  * the values' of the other kernel. */
+/* Byte offsets of what it reads in a raw tile; those of the key's dwords depend on the wavefront's block. */
+struct RebuildPlaces {
+    uint32_t k0, k1, k2, half1, half2, v0, v1, v2, b0, b1, r;
+    int ksh, vsh, bsh; /* the same in all lanes */
+
+    __device__ __forceinline__ void set(int wave, int lane)
+    {
+        /* dword d of a key's string: planes of 16, 16, 12 and 2 bytes per token; of the last half what lies behind it is not looked at */
+        const int bit = PQL_BLOCK_BITS * wave, d0 = bit >> 5;
+        auto key = [&](int d) -> uint32_t {
+            const int base = d < 4 ? PQL_OFF_P0 + 4 * d : (d < 8 ? PQL_OFF_P1 + 4 * (d - 4) : PQL_OFF_P2 + 4 * (d - 8));
+            return (uint32_t)(d < 11 ? base + (d < 8 ? 16 : 12) * lane : PQL_OFF_KP3 + ((2 * lane) & ~3));
+        };
+        auto half = [&](int d) -> uint32_t { return d < 11 ? 0u : 16u * (lane & 1); };
+        k0 = key(d0); k1 = key(d0 + 1); k2 = key(min(d0 + 2, 11));
+        half1 = half(d0 + 1); half2 = half(min(d0 + 2, 11));
+        ksh = bit & 31;
+        /* slots s, s + 1 = 4 i + e0: bits [20 s, 20 s + 40) of the values' string, [6 s, 6 s + 12) of the block indices */
+        const int s = 4 * (wave >> 1) + 2 * (wave & 1), e0 = (20 * s) >> 5;
+        auto value = [&](int d) -> uint32_t {
+            return (uint32_t)(d < 8 ? (d < 4 ? PQL_OFF_P0 + 4 * d : PQL_OFF_P1 + 4 * (d - 4)) + 16 * lane : PQL_OFF_P2 + 4 * (d - 8) + 8 * lane);
+        };
+        v0 = value(e0); v1 = value(min(e0 + 1, 9)); v2 = value(min(e0 + 2, 9));
+        vsh = (20 * s) & 31;
+        const int c0 = (6 * s) >> 5;
+        b0 = (uint32_t)(PQL_OFF_VB + 12 * (lane >> 1) + 4 * c0);
+        b1 = (uint32_t)(PQL_OFF_VB + 12 * (lane >> 1) + 4 * min(c0 + 1, 2));
+        bsh = (6 * s) & 31;
+        r = (uint32_t)(4 * kKeyRadii + 32 * (lane >> 1) + 2 * s);
+    }
+};
+
 template <bool DEEP>
 struct Rebuild {
     uint32_t kx0, kx1, vx0, vx1, vb, kr, vr;
     h2 kq[2], vq[2];   /* radii of the quarters: the key's four, the values' two of each token */
     uint2 kt[4], vt[4];
 
-    /* the strings' dwords; `raw` as in memory */
-    __device__ __forceinline__ void fetch(const uint32_t *rk, const uint32_t *rv, int wave, int lane)
+    /* the strings' dwords; `rk`, `rv` as in memory */
+    __device__ __forceinline__ void fetch(const RawTile &rk, const RawTile &rv, const RebuildPlaces &at, int wave, int lane)
     {
-        /* dword d of a key's string lies at base + stride * token bytes: planes of 16, 16, 12 and 2 bytes per token */
-        const int bit = PQL_BLOCK_BITS * wave, d0 = bit >> 5, sh = bit & 31;
-        const char *k = reinterpret_cast<const char *>(rk), *v = reinterpret_cast<const char *>(rv);
-        auto key_dword = [&](int d) {
-            const int base = d < 4 ? PQL_OFF_P0 + 4 * d : (d < 8 ? PQL_OFF_P1 + 4 * (d - 4) : PQL_OFF_P2 + 4 * (d - 8));
-            const int at = d < 11 ? base + (d < 8 ? 16 : 12) * lane : PQL_OFF_KP3 + ((2 * lane) & ~3);
-            const uint32_t x = *reinterpret_cast<const uint32_t *>(k + at);
-            return d < 11 ? x : x >> (16 * (lane & 1)); /* the last half; behind it nothing is looked at */
-        };
-        const uint32_t w0 = key_dword(d0), w1 = key_dword(d0 + 1), w2 = key_dword(min(d0 + 2, 11));
-        kx0 = __builtin_amdgcn_alignbit(w1, w0, sh);
-        kx1 = __builtin_amdgcn_alignbit(w2, w1, sh);
-        kr = DEEP ? rk[kKeyRadii + lane] : reinterpret_cast<const uint16_t *>(rk + kKeyRadii)[8 * lane + wave];
-        /* slots s, s + 1 = 4 i + e0: bits [20 s, 20 s + 40) of the string, [6 s, 6 s + 12) of the block indices */
-        const int s = 4 * (wave >> 1) + 2 * (wave & 1), e0 = (20 * s) >> 5, vsh = (20 * s) & 31;
-        auto value_dword = [&](int d) {
-            const int at = d < 8 ? (d < 4 ? PQL_OFF_P0 + 4 * d : PQL_OFF_P1 + 4 * (d - 4)) + 16 * lane : PQL_OFF_P2 + 4 * (d - 8) + 8 * lane;
-            return *reinterpret_cast<const uint32_t *>(v + at);
-        };
-        const uint32_t v0 = value_dword(e0), v1 = value_dword(min(e0 + 1, 9)), v2 = value_dword(min(e0 + 2, 9));
-        vx0 = __builtin_amdgcn_alignbit(v1, v0, vsh);
-        vx1 = __builtin_amdgcn_alignbit(v2, v1, vsh);
-        const uint32_t *b = rv + PQL_OFF_VB / 4 + 3 * (lane >> 1);
-        const int b0 = (6 * s) >> 5;
-        vb = __builtin_amdgcn_alignbit(b[min(b0 + 1, 2)], b[b0], (6 * s) & 31);
-        if (!DEEP) vr = *reinterpret_cast<const uint32_t *>(reinterpret_cast<const uint16_t *>(rv + kKeyRadii) + (lane >> 1) * 16 + s);
+        auto dword = [](const RawTile &t, uint32_t o) { return *reinterpret_cast<const uint32_t *>(reinterpret_cast<const char *>(t.w) + o); };
+        const uint32_t w0 = dword(rk, at.k0), w1 = dword(rk, at.k1) >> at.half1, w2 = dword(rk, at.k2) >> at.half2;
+        kx0 = __builtin_amdgcn_alignbit(w1, w0, at.ksh);
+        kx1 = __builtin_amdgcn_alignbit(w2, w1, at.ksh);
+        kr = DEEP ? rk.w[kKeyRadii + lane] : reinterpret_cast<const uint16_t *>(rk.w + kKeyRadii)[8 * lane + wave];
+        const uint32_t v0 = dword(rv, at.v0), v1 = dword(rv, at.v1), v2 = dword(rv, at.v2);
+        vx0 = __builtin_amdgcn_alignbit(v1, v0, at.vsh);
+        vx1 = __builtin_amdgcn_alignbit(v2, v1, at.vsh);
+        vb = __builtin_amdgcn_alignbit(dword(rv, at.b1), dword(rv, at.b0), at.bsh);
+        if (!DEEP) vr = dword(rv, at.r);
     }
 
     /* the tables' entries */
@@ -204,7 +220,11 @@ __global__ __launch_bounds__(kPrefixThreads, 1) void pq_attn_prefix_kernel(Prefi
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int w = (int)blockIdx.x;
+    /* the plan's entries and the row blocks of up to 64 blocks lie in registers, one per lane, requested before anything else */
+    const bool few = a.n_blocks < 64;
     const int total = a.plan[0], working = a.plan[1];
+    const int pre = a.plan[kPlanHeader + min(lane, a.n_blocks)];
+    const BlockRows mine = a.blocks[min(lane, a.n_blocks - 1)];
     {
         const uint32_t *src = a.consts->attn_tab;
         const uint4 t = reinterpret_cast<const uint4 *>(src + PQ_TAB_TQ)[tid];
@@ -218,10 +238,17 @@ __global__ __launch_bounds__(kPrefixThreads, 1) void pq_attn_prefix_kernel(Prefi
     const int base = total / working, rem = total - base * working;
     int gpos = w * base + min(w, rem);
     const int gend = min(gpos + base + (w < rem ? 1 : 0), total);
+    auto prefix_at = [&](int i) { return few ? __builtin_amdgcn_readlane(pre, i) : a.plan[kPlanHeader + i]; };
+    auto rows_of = [&](int i) {
+        if (!few) return a.blocks[i];
+        return BlockRows{__builtin_amdgcn_readlane(mine.group, i), __builtin_amdgcn_readlane(mine.first, i), __builtin_amdgcn_readlane(mine.rows, i),
+                         __builtin_amdgcn_readlane(mine.seq0, i), __builtin_amdgcn_readlane(mine.tokens, i)};
+    };
     /* the last row block whose streams start at or before gpos */
-    int blk = paged_find(a.n_blocks, gpos, lane, [&](int i) { return (int64_t)a.plan[kPlanHeader + i] * a.Hkv; });
+    int blk = few ? __popcll(__ballot(lane <= a.n_blocks && (int64_t)pre * a.Hkv <= gpos)) - 1
+                  : paged_find(a.n_blocks, gpos, lane, [&](int i) { return (int64_t)a.plan[kPlanHeader + i] * a.Hkv; });
     blk = min(max(blk, 0), a.n_blocks - 1);
-    int before = a.plan[kPlanHeader + blk], block_tiles = a.plan[kPlanHeader + blk + 1] - before;
+    int before = prefix_at(blk), block_tiles = prefix_at(blk + 1) - before;
     if (block_tiles <= 0) return; /* cannot happen with a consistent plan */
     int hk, tile_lo;
     {
@@ -229,12 +256,14 @@ __global__ __launch_bounds__(kPrefixThreads, 1) void pq_attn_prefix_kernel(Prefi
         hk = min(r / block_tiles, a.Hkv - 1);
         tile_lo = r - hk * block_tiles;
     }
+    RebuildPlaces places;
+    places.set(wave, lane);
     const int G = a.Hq / a.Hkv;
     constexpr int kRadiiHalves = DEEP ? PQ_DEEP_RADII_HALVES : PQL_RADII;
     const int rg = (wave >> 1) & 3, slice = wave & 1, H = lane >> 5, r32 = lane & 31;
 
     for (;;) { /* one piece per round */
-        const BlockRows rb = a.blocks[blk];
+        const BlockRows rb = rows_of(blk);
         const int tile_hi = min((rb.tokens + 63) >> 6, tile_lo + (gend - gpos));
         const int piece_tiles = tile_hi - tile_lo;
         if (piece_tiles <= 0) return; /* cannot happen with a consistent plan */
@@ -281,6 +310,9 @@ __global__ __launch_bounds__(kPrefixThreads, 1) void pq_attn_prefix_kernel(Prefi
 #pragma unroll
             for (int e = 0; e < 16; ++e) acc[d][e] = 0.f;
         float m_ref = 0.f, l_run = 0.f;
+        f16x start; /* what a tile's scores begin with */
+#pragma unroll
+        for (int e = 0; e < 16; ++e) start[e] = kProbShift;
         bool have_ref = false;
         /* tokens of tile t that are looked at: a tile without a page has none */
         auto tokens_of = [&](int t, int p) { return p < 0 ? 0 : min(rb.tokens - 64 * t, 64); };
@@ -289,7 +321,7 @@ __global__ __launch_bounds__(kPrefixThreads, 1) void pq_attn_prefix_kernel(Prefi
         request((tile_lo + 1) & 1, page1);
         {
             Rebuild<DEEP> r;
-            r.fetch(sRaw[tile_lo & 1][0].w, sRaw[tile_lo & 1][1].w, wave, lane);
+            r.fetch(sRaw[tile_lo & 1][0], sRaw[tile_lo & 1][1], places, wave, lane);
             r.gather(a, tab, sRaw[tile_lo & 1][1].w, wave, tokens_of(tile_lo, page), lane);
             r.store(sK[tile_lo & 1], sV[tile_lo & 1], wave, lane);
         }
@@ -304,15 +336,13 @@ __global__ __launch_bounds__(kPrefixThreads, 1) void pq_attn_prefix_kernel(Prefi
             const int nv = tokens_of(tile, page), nv1 = tokens_of(tile + 1, page1);
             const int lH = l >> 5, lr = l & 31, tok = 32 * slice + lr;
             Rebuild<DEEP> r;
-            r.fetch(sRaw[nxt][0].w, sRaw[nxt][1].w, wave, l);
+            r.fetch(sRaw[nxt][0], sRaw[nxt][1], places, wave, l);
             H8 ko[8];
 #pragma unroll
             for (int ks = 0; ks < 8; ++ks) ko[ks].q = sK[cur][16 * tok + ((2 * ks + lH) ^ (tok & 15))];
             __builtin_amdgcn_sched_barrier(0);
             r.gather(a, tab, sRaw[nxt][1].w, wave, nv1, l);
-            f16x s;
-#pragma unroll
-            for (int e = 0; e < 16; ++e) s[e] = kProbShift - m_ref;
+            f16x s = start;
 #pragma unroll
             for (int ks = 0; ks < 8; ++ks) s = __builtin_amdgcn_mfma_f32_32x32x16_f16(ko[ks].v, q[ks], s, 0, 0, 0);
             __builtin_amdgcn_sched_barrier(0);
@@ -338,7 +368,10 @@ __global__ __launch_bounds__(kPrefixThreads, 1) void pq_attn_prefix_kernel(Prefi
                 m_ref += delta;
                 l_run *= alpha;
 #pragma unroll
-                for (int e = 0; e < 16; ++e) s[e] -= delta;
+                for (int e = 0; e < 16; ++e) {
+                    s[e] -= delta;
+                    start[e] = kProbShift - m_ref;
+                }
 #pragma unroll
                 for (int d = 0; d < 4; ++d) acc[d] *= alpha;
                 have_ref = true;
@@ -411,8 +444,8 @@ __global__ __launch_bounds__(kPrefixThreads, 1) void pq_attn_prefix_kernel(Prefi
             hk = 0;
             do {
                 if (++blk >= a.n_blocks) return;
-                before = a.plan[kPlanHeader + blk];
-                block_tiles = a.plan[kPlanHeader + blk + 1] - before;
+                before = prefix_at(blk);
+                block_tiles = prefix_at(blk + 1) - before;
             } while (block_tiles <= 0);
         }
     }
