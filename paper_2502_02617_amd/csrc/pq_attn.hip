@@ -882,20 +882,13 @@ __global__ __launch_bounds__(WAVES_PER_SIMD * 4 * 64, 1) void pq_attn_partial_ke
         const int64_t piece = (int64_t)w + (int64_t)b * a.Hkv + hk;
 
         /* Descriptors of this sequence's tiles in the four planes (the context is at most 2^31 tokens: 32-bit sizes).  Paged: of the one
-           tile that was requested last, its page out of a register that holds the table's entries of 64 tiles, one per lane. */
+           tile that was requested last; the table's entry of the next one is under way to a scalar register meanwhile.  (Entries of 64
+           tiles in a vector register, and the requests of tiles without a page apart: 33 registers spilled, 65536 tiles 135 us.) */
         __amdgpu_buffer_rsrc_t kc, vc, kr, vr;
-        int page_base = tile_lo;
-        int32_t page_reg = -1;
+        typedef const __attribute__((address_space(4))) int32_t *TableRow; /* nobody writes the table while the kernel runs */
+        const TableRow row = PAGED ? (TableRow)(a.table.pages + (int64_t)b * a.table.ld_pages) : nullptr;
+        int page_ahead = 0;
         bool missing = false; /* the tile requested last has no page */
-        auto fetch_pages = [&](int t) {
-            page_base = t;
-            const int64_t i = (int64_t)b * a.table.ld_pages + min(t + lane, n_tiles - 1);
-            page_reg = a.table.pages[i];
-        };
-        auto page_of = [&](int t) -> int64_t {
-            const int p = __builtin_amdgcn_readlane(page_reg, t - page_base);
-            return p >= 0 && p < a.pool_tiles ? p : -1;
-        };
         auto describe = [&](int64_t tile0, int n) {
             const uint32_t code_bytes = (uint32_t)n * PQL_CODE_BYTES, radii_bytes = (uint32_t)n * (kRadiiHalves * 2u);
             const int64_t at = (int64_t)hk * a.pool_tiles + tile0;
@@ -904,15 +897,15 @@ __global__ __launch_bounds__(WAVES_PER_SIMD * 4 * 64, 1) void pq_attn_partial_ke
             kr = stream_descriptor(a.k_radii + at * kRadiiHalves, radii_bytes);
             vr = stream_descriptor(a.v_radii + at * kRadiiHalves, radii_bytes);
         };
-        if constexpr (PAGED) fetch_pages(tile_lo);
+        if constexpr (PAGED) page_ahead = row[tile_lo];
         else describe(tile0_of(b), n_tiles);
-        /* the number by which tile t is requested from the descriptors: paged, they are set to it first (a tile without a page is
-           requested from the first one of the pool; nobody looks at it) */
+        /* the number by which tile t is requested from the descriptors: paged, they are set to it first, for one tile after the other (a tile
+           without a page is requested from the first one of the pool; nobody looks at it) */
         auto place = [&](int t) -> uint32_t {
             if constexpr (PAGED) {
-                if (t - page_base >= 64) fetch_pages(t);
-                const int64_t p = page_of(t);
-                missing = p < 0;
+                const int p = page_ahead;
+                missing = p < 0 || p >= a.pool_tiles;
+                page_ahead = row[min(t + 1, n_tiles - 1)];
                 describe(missing ? 0 : p, 1);
                 return 0;
             } else {
@@ -966,7 +959,7 @@ __global__ __launch_bounds__(WAVES_PER_SIMD * 4 * 64, 1) void pq_attn_partial_ke
         /* wide: tile `next`'s keys on their way to LDS (behind the last tile: that one again, or none) */
         auto request_keys = [&](int next) {
             if (kInFlight || next < tile_hi) {
-                const uint32_t at = place(min(next, tile_hi - 1)); /* ahead of the descriptors' use */
+                const uint32_t at = PAGED && next >= tile_hi ? 0u : place(min(next, tile_hi - 1)); /* ahead of the descriptors' use */
                 request_k_tile<DEEP>(sK[wave], kc, kr, at, lane);
             }
         };
@@ -1137,16 +1130,11 @@ __global__ __launch_bounds__(WAVES_PER_SIMD * 4 * 64, 1) void pq_attn_partial_ke
         if (WIDE) request_k_tile<DEEP>(sK[wave], kc, kr, at_lo, lane);
         else load_k_tile<DEEP>(kraw, kc, kr, at_lo, lane);
         request_values(tile_lo);
-        /* paged: the tile has no page, its tokens take no part: on to the next one */
-        auto passed_over = [&](int t) {
-            if constexpr (PAGED) {
-                if (missing) {
-                    if (WIDE) request_keys(t + 1);
-                    request_next(t + 1);
-                    return true;
-                }
-            }
-            return false;
+        /* paged: the tokens of a tile without a page take no part */
+        auto tile_or_none = [&](auto masked_c, const int (&lim)[kLanePairs], int nv, int t) {
+            if (!PAGED || !missing) do_tile(masked_c, kraw, vraw, lim, nv, t + 1);
+            else if (WIDE) request_keys(t + 1);
+            request_next(t + 1);
         };
         int tile = tile_lo;
         {
@@ -1165,13 +1153,10 @@ __global__ __launch_bounds__(WAVES_PER_SIMD * 4 * 64, 1) void pq_attn_partial_ke
                     const int ahead = (d4.x > done) + (d4.y > done) + (d4.z > done) + (d4.w > done);
                     set_wave_priority(min(__builtin_amdgcn_readfirstlane(ahead), 3));
                 }
-                if (passed_over(tile)) continue;
-                do_tile(std::false_type{}, kraw, vraw, lim, 64, tile + 1);
-                request_next(tile + 1);
+                tile_or_none(std::false_type{}, lim, 64, tile);
             }
         }
         for (; tile < tile_hi; ++tile) { /* the masked tiles at the end of the sequence */
-            if (passed_over(tile)) continue;
             const int nv = min(ctx - tile * 64, 64);
             int lim[kLanePairs]; /* tokens of this tile that the pair may see */
 #pragma unroll
@@ -1179,8 +1164,7 @@ __global__ __launch_bounds__(WAVES_PER_SIMD * 4 * 64, 1) void pq_attn_partial_ke
                 const int m = WIDE ? m_q : (h < a.M * G ? h / G : 0);
                 lim[h] = ctx - (a.M - 1 - m) - tile * 64;
             }
-            do_tile(std::true_type{}, kraw, vraw, lim, nv, tile + 1);
-            request_next(tile + 1);
+            tile_or_none(std::true_type{}, lim, nv, tile);
         }
 
         if (kInFlight) keys_arrived<DEEP>(); /* the last tile's, requested again: nothing writes to LDS any more */
