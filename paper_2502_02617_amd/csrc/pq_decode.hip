@@ -204,20 +204,33 @@ __device__ __forceinline__ void dq_store_pair(void *out, int64_t at, float a, fl
  * travels under the rebuild and the products of this half tile.  (Values spill one register to bf16 and three with AHEAD, keys
  * one with AHEAD; measured as they are.)  Whole tiles on eight wavefronts of 256 registers (S fetched half as often)
  * spill 100 registers; value slots are read from an image in LDS because a token's 16 slots are spread over 16 strings. */
-template <int KIND, int OT, bool UNIT, bool AHEAD, bool PAGED>
-__global__ __launch_bounds__(kDecodeThreads, 1) void pq_decode_kernel(DecodeArgs a)
+constexpr int kDecodeChunks = 4 * 8 * 64; /* of S, of eight halves: (64-coordinate group, parity), k-step, lane */
+
+template <bool UNIT, bool IMAGE>
+struct DecodeLds {
+    uint4 sS[(UNIT ? 1 : 2) * kDecodeChunks];
+    __attribute__((aligned(16))) float tq[2][64][2], tb[64][4];
+    float2 tup[24];
+    __attribute__((aligned(16))) float sUn[kDecodeWaves][32];
+    __attribute__((aligned(16))) uint32_t img[IMAGE ? kDecodeWaves : 1][IMAGE ? kTileDwords : 4];
+};
+
+/* The half tiles of workgroup `block` of `n_blocks` */
+template <int KIND, int OT, bool UNIT, bool AHEAD, bool PAGED, typename Lds>
+__device__ __forceinline__ void decode_half_tiles(const DecodeArgs &a, Lds &lds, int block, int n_blocks)
 {
-    constexpr int kChunks = 4 * 8 * 64; /* of eight halves: (64-coordinate group, parity), k-step, lane */
-    __shared__ uint4 sS[(UNIT ? 1 : 2) * kChunks];
-    __shared__ __attribute__((aligned(16))) float tq[2][64][2], tb[64][4];
-    __shared__ float2 tup[24];
-    __shared__ __attribute__((aligned(16))) float sUn[kDecodeWaves][32];
-    __shared__ __attribute__((aligned(16))) uint32_t img[AHEAD || KIND == PQ_VALUE ? kDecodeWaves : 1][AHEAD || KIND == PQ_VALUE ? kTileDwords : 4];
+    constexpr int kChunks = kDecodeChunks;
+    auto &sS = lds.sS;
+    auto &tq = lds.tq;
+    auto &tb = lds.tb;
+    auto &tup = lds.tup;
+    auto &sUn = lds.sUn;
+    auto &img = lds.img;
     const int tid = threadIdx.x;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const PqDeviceConsts &K = *a.consts;
     /* consecutive half tiles go to different workgroups: a short range occupies every CU */
-    const int64_t stride = (int64_t)kDecodeWaves * gridDim.x;
+    const int64_t stride = (int64_t)kDecodeWaves * n_blocks;
     const int radii_halves = a.deep ? PQ_DEEP_RADII_HALVES : PQL_RADII;
     auto place = [&](int64_t tile_in, int lane) {
         if constexpr (PAGED) {
@@ -230,7 +243,7 @@ __global__ __launch_bounds__(kDecodeThreads, 1) void pq_decode_kernel(DecodeArgs
         const int64_t at = head * a.pool_tiles + max(place(full_tile - head * a.n_tiles, lane).tile, (int64_t)0);
         dq_request_tile(img[wave], a.codes + at * PQL_CODE_BYTES, a.radii + at * radii_halves, 2 * radii_halves, lane);
     };
-    int64_t item = (int64_t)wave * gridDim.x + blockIdx.x;
+    int64_t item = (int64_t)wave * n_blocks + block;
     /* The wavefront's first tile is under way to LDS while S is staged (without, values to bf16: 12000 tokens of 8 heads 17.6
        instead of 17.2 us, 3000 of 8 9.8 instead of 9.6; 32768 of 8 within the spread, 35.2 and 35.4). */
     bool requested = KIND == PQ_VALUE || AHEAD;
@@ -412,6 +425,22 @@ __global__ __launch_bounds__(kDecodeThreads, 1) void pq_decode_kernel(DecodeArgs
     }
 }
 
+template <int KIND, int OT, bool UNIT, bool AHEAD>
+__global__ __launch_bounds__(kDecodeThreads, 1) void pq_decode_kernel(DecodeArgs a)
+{
+    __shared__ DecodeLds<UNIT, AHEAD || KIND == PQ_VALUE> lds;
+    decode_half_tiles<KIND, OT, UNIT, AHEAD, false>(a, lds, (int)blockIdx.x, (int)gridDim.x);
+}
+
+/* ragged rows of a paged cache: keys on workgroups [0, k_blocks), values on the rest */
+template <int OT, bool UNIT>
+__global__ __launch_bounds__(kDecodeThreads, 1) void pq_decode_paged_kernel(DecodeArgs k, DecodeArgs v, int k_blocks)
+{
+    __shared__ DecodeLds<UNIT, true> lds;
+    if ((int)blockIdx.x < k_blocks) decode_half_tiles<PQ_KEY, OT, UNIT, false, true>(k, lds, (int)blockIdx.x, k_blocks);
+    else decode_half_tiles<PQ_VALUE, OT, UNIT, false, true>(v, lds, (int)blockIdx.x - k_blocks, (int)gridDim.x - k_blocks);
+}
+
 /* DeQuant without the trailing S^T: sixteen tokens per workgroup, a thread per (token, block) rebuilds its sixteen
  * coordinates, and every row is then written by the 128 threads as whole lines; any strides.  Bound by the generic reader's
  * loads and the stores: 262144 vectors to bf16 36 us for keys, 38 for values, to fp32 62 and 64.  (Stored by the kernel above
@@ -479,18 +508,20 @@ void launch_decode(const DecodeArgs &a, bool unit, int rotated, int n_heads, hip
        LDS pass costs; 3001 fp32 keys 11.1 / 10.6). */
     const bool ahead = OT == PQ_F32 && a.n_items > 256 * kDecodeWaves;
     if constexpr (OT == PQ_F32)
-        if (ahead) return unit ? launch(pq_decode_kernel<KIND, OT, true, true, false>) : launch(pq_decode_kernel<KIND, OT, false, true, false>);
-    if (unit) launch(pq_decode_kernel<KIND, OT, true, false, false>);
-    else launch(pq_decode_kernel<KIND, OT, false, false, false>);
+        if (ahead) return unit ? launch(pq_decode_kernel<KIND, OT, true, true>) : launch(pq_decode_kernel<KIND, OT, false, true>);
+    if (unit) launch(pq_decode_kernel<KIND, OT, true, false>);
+    else launch(pq_decode_kernel<KIND, OT, false, false>);
 }
 
-template <int KIND, int OT>
-void launch_decode_paged(const DecodeArgs &a, bool unit, hipStream_t s)
+/* one workgroup per CU, half of them for either kind */
+template <int OT>
+void launch_decode_paged(const DecodeArgs &k, const DecodeArgs &v, bool unit, hipStream_t s)
 {
-    const dim3 grid((unsigned)(a.n_items < 256 ? a.n_items : 256));
-    auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(kDecodeThreads), 0, s, a); };
-    if (unit) launch(pq_decode_kernel<KIND, OT, true, false, true>);
-    else launch(pq_decode_kernel<KIND, OT, false, false, true>);
+    const unsigned most = k.out && v.out ? 128u : 256u, per_kind = k.n_items < most ? (unsigned)k.n_items : most;
+    const unsigned k_blocks = k.out ? per_kind : 0u, v_blocks = v.out ? per_kind : 0u;
+    auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(k_blocks + v_blocks), dim3(kDecodeThreads), 0, s, k, v, (int)k_blocks); };
+    if (unit) launch(pq_decode_paged_kernel<OT, true>);
+    else launch(pq_decode_paged_kernel<OT, false>);
 }
 
 struct ExportArgs {
@@ -638,16 +669,11 @@ extern "C" pq_status pq_decode_paged(const pq_ctx *ctx, const uint8_t *k_codes, 
     a.table = PagedTable{pages, ld_pages, pool_tokens / 64};
     a.rows = PagedRows{row_start, ctx_len, n_seq, n_rows};
     hipStream_t s = static_cast<hipStream_t>(hip_stream);
-    if (out_k) {
-        a.codes = k_codes; a.radii = k_radii; a.out = out_k;
-        if (ot == PQ_F32) launch_decode_paged<PQ_KEY, PQ_F32>(a, ctx->unit_entries, s);
-        else launch_decode_paged<PQ_KEY, PQ_BF16>(a, ctx->unit_entries, s);
-    }
-    if (out_v) {
-        a.codes = v_codes; a.radii = v_radii; a.out = out_v;
-        if (ot == PQ_F32) launch_decode_paged<PQ_VALUE, PQ_F32>(a, ctx->unit_entries, s);
-        else launch_decode_paged<PQ_VALUE, PQ_BF16>(a, ctx->unit_entries, s);
-    }
+    DecodeArgs v = a;
+    a.codes = k_codes; a.radii = k_radii; a.out = out_k;
+    v.codes = v_codes; v.radii = v_radii; v.out = out_v;
+    if (ot == PQ_F32) launch_decode_paged<PQ_F32>(a, v, ctx->unit_entries, s);
+    else launch_decode_paged<PQ_BF16>(a, v, ctx->unit_entries, s);
     PQ_HIP_TRY(hipGetLastError());
     return PQ_OK;
 }
