@@ -96,6 +96,13 @@ __device__ __forceinline__ uint16_t radius_exact(double q)
     return __builtin_bit_cast(uint16_t, (_Float16)fmin(sqrt(q), 65504.0));
 }
 
+/* x of the lane that the DPP control names, inside rows of sixteen lanes */
+template <int CTRL>
+__device__ __forceinline__ double dpp_double(double x)
+{
+    return __hiloint2double(pq_dpp<CTRL>(__double2hiint(x)), pq_dpp<CTRL>(__double2loint(x)));
+}
+
 __device__ __forceinline__ double shfl_xor_double(double x, int d)
 {
     const int lo = __shfl_xor(__double2loint(x), d), hi = __shfl_xor(__double2hiint(x), d);
@@ -111,11 +118,11 @@ __device__ __forceinline__ void write_exact(const AppendPagedArgs &a, const Exac
     const PqDeviceConsts &K = *a.consts;
     const int i = lane & 7, b = lane >> 3;
     const uint32_t code1 = level1_exact(ya, yb, E, B);
-    const double q1 = ya * ya + yb * yb, q1s = shfl_xor_double(q1, 1);
+    const double q1 = ya * ya + yb * yb, q1s = dpp_double<0xB1>(q1); /* lane ^ 1 */
     const uint32_t c2 = quant3_exact(q1, q1s, B.tan2[0]);
-    const double q2 = q1 + q1s, q2s = shfl_xor_double(q2, 2);
+    const double q2 = q1 + q1s, q2s = dpp_double<0x4E>(q2); /* lane ^ 2 */
     const uint32_t c3 = quant3_exact(q2, q2s, B.tan2[1]);
-    const double q3 = q2 + q2s, q3s = shfl_xor_double(q3, 4);
+    const double q3 = q2 + q2s, q3s = dpp_double<0x141>(q3); /* lane 7 - i of eight: any lane of the other quad */
     PqBlockFields f;
     f.c4 = quant3_exact(q3, q3s, B.tan2[2]);
     const double q4 = q3 + q3s;
@@ -123,11 +130,9 @@ __device__ __forceinline__ void write_exact(const AppendPagedArgs &a, const Exac
     /* level-1 codes at their nibbles; [c2(2h) | c3(h) | c2(2h+1)] of half-block h at bits [8 h, 8 h + 6) */
     uint32_t l1 = code1 << (4 * i);
     uint32_t gw = (i & 1) ? 0u : ((i & 2) ? c2 : ((c2 << 4) | (c3 << 2))) << (2 * (i & 4));
-#pragma unroll
-    for (int d = 1; d < 8; d <<= 1) {
-        l1 |= __shfl_xor(l1, d);
-        gw |= __shfl_xor(gw, d);
-    }
+    l1 |= pq_dpp<0xB1>(l1); gw |= pq_dpp<0xB1>(gw);
+    l1 |= pq_dpp<0x4E>(l1); gw |= pq_dpp<0x4E>(gw);
+    l1 |= pq_dpp<0x141>(l1); gw |= pq_dpp<0x141>(gw);
     f.l1 = l1;
     f.g6[0] = gw & 63u;
     f.g6[1] = (gw >> 8) & 63u;
@@ -164,27 +169,33 @@ struct ExactSlice {
     }
 };
 
+template <int NV>
 struct ExactLds {
-    double x[4][PQ_D];
-    double part[4][4][PQ_D];
+    __attribute__((aligned(16))) double x[NV][PQ_D];
+    double part[NV][4][PQ_D];
 };
 
-template <int NV>
-__device__ __forceinline__ void multiply_exact(const ExactSlice &s, ExactLds &lds, int tid)
+template <int NV, typename Lds>
+__device__ __forceinline__ void multiply_exact(const ExactSlice &s, Lds &lds, int tid)
 {
     const int kq = tid >> 7, j = tid & 127;
     double acc[NV];
 #pragma unroll
     for (int v = 0; v < NV; ++v) acc[v] = 0.0;
 #pragma unroll
-    for (int k = 0; k < 32; ++k)
+    for (int k = 0; k < 32; k += 2)
 #pragma unroll
-        for (int v = 0; v < NV; ++v) acc[v] = fma(lds.x[v][32 * kq + k], s.m[k], acc[v]);
+        for (int v = 0; v < NV; ++v) {
+            const double2 x = *reinterpret_cast<const double2 *>(&lds.x[v][32 * kq + k]);
+            acc[v] = fma(x.x, s.m[k], acc[v]);
+            acc[v] = fma(x.y, s.m[k + 1], acc[v]);
+        }
 #pragma unroll
     for (int v = 0; v < NV; ++v) lds.part[v][kq][j] = acc[v];
 }
 
-__device__ __forceinline__ double rotated_exact(const ExactLds &lds, int r, int c)
+template <typename Lds>
+__device__ __forceinline__ double rotated_exact(const Lds &lds, int r, int c)
 {
     return ((lds.part[r][0][c] + lds.part[r][1][c]) + lds.part[r][2][c]) + lds.part[r][3][c];
 }
@@ -210,7 +221,7 @@ __device__ __forceinline__ double element_exact(const AppendPagedArgs &a, int ki
 /* NV vectors (row, head) of kind KIND by one workgroup of 512 threads, vec0 .. vec0 + NV - 1 as far as they are below n_vec; wavefronts
  * 2 r and 2 r + 1 fetch vector r, the first of them runs its recursion. */
 template <int XT, int KIND, int NV>
-__device__ __forceinline__ void append_vectors_exact(const AppendPagedArgs &a, int64_t vec0, int64_t n_vec, ExactLds &lds)
+__device__ __forceinline__ void append_vectors_exact(const AppendPagedArgs &a, int64_t vec0, int64_t n_vec, ExactLds<NV> &lds)
 {
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     ExactSlice s;
@@ -234,7 +245,7 @@ __device__ __forceinline__ void append_vectors_exact(const AppendPagedArgs &a, i
 template <int XT, int NV>
 __global__ __launch_bounds__(512) void pq_append_paged_kernel(AppendPagedArgs a, int64_t n_vec, int n_blocks)
 {
-    __shared__ ExactLds lds;
+    __shared__ ExactLds<NV> lds;
     const int blk = (int)blockIdx.x;
     if (blk < n_blocks) append_vectors_exact<XT, PQ_KEY, NV>(a, (int64_t)NV * blk, n_vec, lds);
     else append_vectors_exact<XT, PQ_VALUE, NV>(a, (int64_t)NV * (blk - n_blocks), n_vec, lds);
@@ -244,15 +255,15 @@ __global__ __launch_bounds__(512) void pq_append_paged_kernel(AppendPagedArgs a,
  * A workgroup per tile, as for short inputs of pq_encode_kv: rows are rotated in fp32 and left in LDS as matrix operands, eight threads
  * per vector; wavefront (v, rt) multiplies the 32 vectors of half v into row tile rt of S and runs the recursion of blocks rt and 4 + rt.
  *
- * Codes in doubt.  A rotated coordinate is off by less than E = 2^-22 |x|: 24 products of matrix instructions add to one fp32 sum, whose
- * roundings are 2^-24 of partial sums far below |x|; with 2^-24 in place of 2^-22 no code of 2 * 10^9 was wrong, with 2^-26 13 were, and
+ * Codes in doubt.  A rotated coordinate is off by less than E = 2^-23 |x|: 24 products of matrix instructions add to one fp32 sum, whose
+ * roundings are 2^-24 of partial sums far below |x|; with 2^-24 in place of 2^-23 no code of 2 * 10^9 was wrong, with 2^-26 13 were, and
  * without any doubt 326.  The code of a node is certain if its inputs u, v are further from every boundary t than that moves the
  * comparison: |tan t u - v| > (1 + tan t) E at level 1, where a coordinate's sign is a boundary as well; above it, where squares are
  * compared, |tan^2 t u^2 - v^2| > 2 sqrt 2 E |(u, v)| sin t (1 + tan t).  The largest factor of a level's boundaries serves for all, and
  * |(u, v)| is bounded from above by (q / s + s) / 2, q = u^2 + v^2, with s the node's usual radius: doubt is only ever found too often, in 1 of
- * 250 vectors without a preferred direction.  The workgroup lists them and, behind its last tile, codes them once more in 64 bits, four
- * at a time. */
-constexpr float kDoubt = 0x1p-22f;
+ * 500 vectors without a preferred direction.  The workgroup lists them and, behind its last tile, codes them once more in 64 bits, eight at a
+ * time, a wavefront each (5 us; four at a time, twice as many in doubt: 8192 tokens of 8 heads 46 us, now 41). */
+constexpr float kDoubt = 0x1p-23f;
 constexpr int kChunkItems = 256; /* tiles of one workgroup at most */
 constexpr int kListed = 256;     /* vectors that are coded once more in one go */
 
@@ -370,7 +381,7 @@ __global__ __launch_bounds__(512) void pq_append_chunk_kernel(AppendPagedArgs a,
     constexpr int kRaw = XT == PQ_BF16 ? 2 : 4;
     __shared__ union {
         uint4 rows[2 * kRows];
-        ExactLds exact;
+        ExactLds<8> exact;
     } lds;
     __shared__ __align__(16) uint32_t sImg[2][kWaveDwords];
     __shared__ float sQ4[DEEP ? 2 : 1][2][4][DEEP ? 64 : 1];
@@ -671,7 +682,7 @@ __global__ __launch_bounds__(512) void pq_append_chunk_kernel(AppendPagedArgs a,
     }
     ++n_done;
 
-    /* ---- the vectors in doubt in 64 bits, four per turn.  More than the list holds: lists are made from the marks, 256 vectors at a time. ---- */
+    /* ---- the vectors in doubt in 64 bits, one per wavefront and turn.  More than the list holds: lists are made from the marks, 256 vectors at a time. ---- */
     __syncthreads(); /* the workgroup's stores of whole tiles come before its updates of single fields */
     const int in_doubt = sCount;
     for (int skip = 0; skip < in_doubt; skip += kListed) {
@@ -695,23 +706,27 @@ __global__ __launch_bounds__(512) void pq_append_chunk_kernel(AppendPagedArgs a,
             }
             __syncthreads();
         }
-        const int n = min(in_doubt - skip, kListed), r = wave >> 1;
-        for (int k = 0; k < n; k += 4) {
+        const int n = min(in_doubt - skip, kListed);
+        for (int k = 0; k < n; k += 8) {
             ExactSlice s;
             s.load(a.exact->S, tid);
             ExactBounds bounds;
             bounds.load(*a.exact, *a.consts);
-            const uint32_t entry = __builtin_amdgcn_readfirstlane(sList[min(k + r, n - 1)]);
+            const uint32_t entry = __builtin_amdgcn_readfirstlane(sList[min(k + wave, n - 1)]);
             const ChunkItem ci = sItem[entry >> 6];
             const int slot = (int)(entry & 63u), kind = ci.head_kind & 1, head = ci.head_kind >> 1;
-            const int64_t row = (int64_t)ci.row0 + slot;
+            const int64_t row = (int64_t)ci.row0 + slot, off = row * a.ld_token + (int64_t)head * a.ld_head;
             const int64_t position = a.positions ? (int64_t)a.positions[row] : (int64_t)ci.token0 + slot;
-            lds.exact.x[r][tid & 127] = element_exact<XT>(a, kind, row * a.ld_token + (int64_t)head * a.ld_head, position, tid & 127);
+            const double x0 = element_exact<XT>(a, kind, off, position, lane), x1 = element_exact<XT>(a, kind, off, position, lane + 64);
+            lds.exact.x[wave][lane] = x0;
+            lds.exact.x[wave][lane + 64] = x1;
             __syncthreads();
-            multiply_exact<4>(s, lds.exact, tid);
+            if (n - k == 1) multiply_exact<1>(s, lds.exact, tid);
+            else if (n - k <= 4) multiply_exact<4>(s, lds.exact, tid);
+            else multiply_exact<8>(s, lds.exact, tid);
             __syncthreads();
-            if ((wave & 1) == 0 && k + r < n) {
-                const double ya = rotated_exact(lds.exact, r, 2 * lane), yb = rotated_exact(lds.exact, r, 2 * lane + 1);
+            if (k + wave < n) {
+                const double ya = rotated_exact(lds.exact, wave, 2 * lane), yb = rotated_exact(lds.exact, wave, 2 * lane + 1);
                 const int64_t tile = (int64_t)head * a.table.pool_pages + ci.page;
                 if (kind == PQ_KEY) write_exact<PQ_KEY>(a, bounds, ya, yb, tile, slot, lane);
                 else write_exact<PQ_VALUE>(a, bounds, ya, yb, tile, slot, lane);
