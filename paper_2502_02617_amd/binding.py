@@ -189,13 +189,18 @@ def _stream():
 
 
 def _dtype_code(t):
-    import torch
+    global _dtype_codes
+    if _dtype_codes is None:
+        import torch
 
-    if t.dtype == torch.bfloat16:
-        return PQ_BF16
-    if t.dtype == torch.float32:
-        return PQ_F32
-    raise PolarQuantError("only float32 and bfloat16 tensors are supported")
+        _dtype_codes = {torch.bfloat16: PQ_BF16, torch.float32: PQ_F32}
+    code = _dtype_codes.get(t.dtype)
+    if code is None:
+        raise PolarQuantError("only float32 and bfloat16 tensors are supported")
+    return code
+
+
+_dtype_codes = None
 
 
 class Rotary(ctypes.Structure):
@@ -213,24 +218,37 @@ class Rotary(ctypes.Structure):
         self.cos_sin, self.n_pos, self.dim, self.interleaved = cos_sin.data_ptr(), cos_sin.shape[0], cos_sin.shape[1], int(bool(interleaved))
 
 
-def _ints(name, t, shape):
-    """Address of an int32 device tensor of that shape (a row of `pages` may be longer than it is read), rows contiguous."""
-    import torch
+def _int32():
+    """torch.int32, without an import statement in the path of a call (0.4 us)."""
+    global _int32_type
+    if _int32_type is None:
+        import torch
 
-    if t.dtype != torch.int32 or not t.is_cuda or tuple(t.shape) != tuple(shape) or (t.dim() and t.shape[-1] > 1 and t.stride(-1) != 1):
-        raise PolarQuantError(f"{name} must be an int32 device tensor of shape {list(shape)}, innermost dimension contiguous")
+        _int32_type = torch.int32
+    return _int32_type
+
+
+_int32_type = None
+
+
+def _ints(name, t, n):
+    """Address of an int32 device vector of n entries."""
+    if t.dtype is not _int32() or not t.is_cuda or t.dim() != 1 or t.shape[0] != n or (n > 1 and t.stride(0) != 1):
+        raise PolarQuantError(f"{name} must be a contiguous int32 device tensor of {n} entries")
     return t.data_ptr()
 
 
-def _pages(pages, n_seq):
-    if pages.dim() != 2:
-        raise PolarQuantError("pages must be [n_seq, pages per sequence]")
-    at = _ints("pages", pages, (n_seq, pages.shape[1]))
-    return at, int(pages.stride(0)) if n_seq > 1 else int(pages.shape[1])
+def _pages(t, n_seq):
+    """Address and row length of a page table."""
+    if t.dtype is not _int32() or not t.is_cuda or t.dim() != 2 or t.shape[0] != n_seq or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise PolarQuantError(f"pages must be an int32 device tensor [{n_seq}, pages of a sequence], rows contiguous")
+    return t.data_ptr(), t.stride(0) if n_seq > 1 else t.shape[1]
 
 
 class Context:
     """pq_ctx: the preconditioner S, the codebooks and the device constant tables."""
+
+    _radii_halves = TILE_RADII  # of a tile, in this context's format
 
     def __init__(self, seed=0, S=None, d=D, hadamard=False):
         """S: explicit d x d orthogonal matrix; hadamard=True: randomised Hadamard matrix from seed
@@ -281,6 +299,7 @@ class Context:
             if bits.size != 3:
                 raise PolarQuantError("upper_bits must hold 3 widths")
         _check(library().pq_set_recursion_depth(self._h, int(depth), bits.ctypes.data_as(ctypes.c_void_p) if bits is not None else None))
+        self._radii_halves = self.radii_halves_per_tile()
 
     def set_upper_codebooks(self, cbt):
         """Centroids of levels 5, 6, 7 of a depth-7 context, array [3, 8] (2^bits used per row); before the first launch."""
@@ -536,51 +555,51 @@ class Context:
     def _paged_cache(self, k_codes, k_radii, v_codes, v_radii):
         """Checks the four buffers of a cache in this context's format -> (head planes, slots of a plane)."""
         heads, tiles = k_codes.shape[0], k_codes.shape[1]
-        halves = self.radii_halves_per_tile()
-        for t, last in ((k_codes, TILE_CODE_BYTES), (v_codes, TILE_CODE_BYTES), (k_radii, halves), (v_radii, halves)):
-            if tuple(t.shape) != (heads, tiles, last) or not t.is_contiguous() or not t.is_cuda:
-                raise PolarQuantError("the cache must be as alloc_cache_for makes it, keys and values of one size")
+        codes, radii = (heads, tiles, TILE_CODE_BYTES), (heads, tiles, self._radii_halves)
+        if not (k_codes.shape == codes and v_codes.shape == codes and k_radii.shape == radii and v_radii.shape == radii
+                and k_codes.is_contiguous() and v_codes.is_contiguous() and k_radii.is_contiguous() and v_radii.is_contiguous()
+                and k_codes.is_cuda and v_codes.is_cuda and k_radii.is_cuda and v_radii.is_cuda
+                and k_codes.element_size() == 1 and v_codes.element_size() == 1 and k_radii.element_size() == 2 and v_radii.element_size() == 2):
+            raise PolarQuantError("the cache must be device tensors as alloc_cache_for makes them, keys and values of one size")
         return heads, tiles * TILE_TOKENS
 
     def append_paged(self, xk, xv, row_start, ctx_len, k_codes, k_radii, v_codes, v_radii, pages, rotary=None, positions=None):
         """xk, xv: [rows, n_heads, 128] of one shape, dtype and strides (views of a projection's output, say); row_start int32
         [n_seq + 1], ctx_len int32 [n_seq] (new tokens counted), pages int32 [n_seq, pages]; rotary: Rotary for the keys, positions
         int32 [rows] or None."""
-        if xk.dim() != 3 or xk.shape != xv.shape or xk.stride() != xv.stride() or xk.dtype != xv.dtype:
-            raise PolarQuantError("xk and xv must be [rows, n_heads, 128] of one shape, dtype and strides")
-        if xk.shape[2] != D or xk.stride(2) != 1 or not (xk.is_cuda and xv.is_cuda):
-            raise PolarQuantError("xk and xv must be device tensors with 128 contiguous coordinates")
+        shape, stride = xk.shape, xk.stride()
         heads, pool_tokens = self._paged_cache(k_codes, k_radii, v_codes, v_radii)
-        if xk.shape[1] != heads:
-            raise PolarQuantError("xk and the cache differ in heads")
-        n_seq = ctx_len.shape[0]
+        if len(shape) != 3 or shape != xv.shape or stride != xv.stride() or xk.dtype != xv.dtype or shape[1] != heads or shape[2] != D or stride[2] != 1 \
+                or not (xk.is_cuda and xv.is_cuda):
+            raise PolarQuantError("xk and xv must be device tensors [rows, n_heads, 128] of one shape, dtype and strides, coordinates contiguous, "
+                                  "with the cache's heads")
+        n_rows, n_seq = shape[0], ctx_len.shape[0]
         table, ld = _pages(pages, n_seq)
         _check(library().pq_append_paged(
-            self._h, xk.data_ptr(), xv.data_ptr(), _dtype_code(xk), int(xk.shape[0]), heads, int(xk.stride(0)), int(xk.stride(1)),
-            ctypes.byref(rotary) if rotary is not None else None,
-            _ints("positions", positions, (xk.shape[0],)) if positions is not None else None,
+            self._h, xk.data_ptr(), xv.data_ptr(), _dtype_code(xk), n_rows, heads, stride[0], stride[1],
+            ctypes.addressof(rotary) if rotary is not None else None, _ints("positions", positions, n_rows) if positions is not None else None,
             k_codes.data_ptr(), k_radii.data_ptr(), v_codes.data_ptr(), v_radii.data_ptr(), pool_tokens, table, ld,
-            _ints("row_start", row_start, (n_seq + 1,)), _ints("ctx_len", ctx_len, (n_seq,)), int(n_seq), _stream()))
+            _ints("row_start", row_start, n_seq + 1), _ints("ctx_len", ctx_len, n_seq), n_seq, _stream()))
 
     def decode_paged(self, k_codes, k_radii, v_codes, v_radii, pages, row_start, ctx_len, out_k=None, out_v=None):
         """out_k, out_v: [rows, n_heads, 128] float32 or bfloat16, of one shape, dtype and strides, or one of them None."""
         o = out_k if out_k is not None else out_v
         if o is None:
             raise PolarQuantError("give out_k, out_v or both")
-        for t in (out_k, out_v):
-            if t is not None and (t.dim() != 3 or t.shape != o.shape or t.stride() != o.stride() or t.dtype != o.dtype or t.shape[2] != D
-                                  or t.stride(2) != 1 or not t.is_cuda):
-                raise PolarQuantError("out_k and out_v must be [rows, n_heads, 128] device tensors of one shape, dtype and strides")
+        shape, stride = o.shape, o.stride()
         heads, pool_tokens = self._paged_cache(k_codes, k_radii, v_codes, v_radii)
-        if o.shape[1] != heads:
-            raise PolarQuantError("the outputs and the cache differ in heads")
+        if len(shape) != 3 or shape[1] != heads or shape[2] != D or stride[2] != 1 or not o.is_cuda or \
+                (out_k is not None and out_v is not None
+                 and (out_v.shape != shape or out_v.stride() != stride or out_v.dtype != out_k.dtype or not out_v.is_cuda)):
+            raise PolarQuantError("out_k and out_v must be device tensors [rows, n_heads, 128] of one shape, dtype and strides, coordinates contiguous, "
+                                  "with the cache's heads")
         n_seq = ctx_len.shape[0]
         table, ld = _pages(pages, n_seq)
         _check(library().pq_decode_paged(
             self._h, k_codes.data_ptr(), k_radii.data_ptr(), v_codes.data_ptr(), v_radii.data_ptr(), pool_tokens, table, ld,
-            _ints("row_start", row_start, (n_seq + 1,)), _ints("ctx_len", ctx_len, (n_seq,)), int(n_seq), int(o.shape[0]), heads,
+            _ints("row_start", row_start, n_seq + 1), _ints("ctx_len", ctx_len, n_seq), n_seq, shape[0], heads,
             out_k.data_ptr() if out_k is not None else None, out_v.data_ptr() if out_v is not None else None, _dtype_code(o),
-            int(o.stride(0)), int(o.stride(1)), _stream()))
+            stride[0], stride[1], _stream()))
 
     def attn_paged(self, q, out, k_codes, k_radii, v_codes, v_radii, pages, ctx_len, max_ctx, softmax_scale, workspace, rotary=None,
                    positions=None):
@@ -590,10 +609,10 @@ class Context:
         heads, pool_tokens = self._paged_cache(k_codes, k_radii, v_codes, v_radii)
         table, ld = _pages(pages, B)
         _check(library().pq_attn_paged(
-            self._h, q.data_ptr(), out.data_ptr(), _dtype_code(out), ctypes.byref(rotary) if rotary is not None else None,
+            self._h, q.data_ptr(), out.data_ptr(), _dtype_code(out), ctypes.addressof(rotary) if rotary is not None else None,
             self._query_positions(positions, B, M), k_codes.data_ptr(), k_radii.data_ptr(), v_codes.data_ptr(), v_radii.data_ptr(),
-            pool_tokens, table, ld, _ints("ctx_len", ctx_len, (B,)), B, M, Hq, heads, int(max_ctx), float(softmax_scale),
-            workspace.data_ptr(), int(workspace.numel() * workspace.element_size()), _stream()))
+            pool_tokens, table, ld, _ints("ctx_len", ctx_len, B), B, M, Hq, heads, max_ctx, softmax_scale,
+            workspace.data_ptr(), workspace.numel() * workspace.element_size(), _stream()))
 
     def attn_prefix_paged(self, q, out, k_codes, k_radii, v_codes, v_radii, pages, ctx_len, max_ctx, prefix_pages, prefix_len, group_start,
                           max_prefix, softmax_scale, workspace, rotary=None, positions=None):
@@ -605,11 +624,11 @@ class Context:
         n_groups = prefix_len.shape[0]
         pre_table, pre_ld = _pages(prefix_pages, n_groups)
         _check(library().pq_attn_prefix_paged(
-            self._h, q.data_ptr(), out.data_ptr(), _dtype_code(out), ctypes.byref(rotary) if rotary is not None else None,
+            self._h, q.data_ptr(), out.data_ptr(), _dtype_code(out), ctypes.addressof(rotary) if rotary is not None else None,
             self._query_positions(positions, B, M), k_codes.data_ptr(), k_radii.data_ptr(), v_codes.data_ptr(), v_radii.data_ptr(),
-            pool_tokens, table, ld, _ints("ctx_len", ctx_len, (B,)), B, M, Hq, heads, int(max_ctx), pre_table, pre_ld,
-            _ints("prefix_len", prefix_len, (n_groups,)), _ints("group_start", group_start, (n_groups + 1,)), int(n_groups), int(max_prefix),
-            float(softmax_scale), workspace.data_ptr(), int(workspace.numel() * workspace.element_size()), _stream()))
+            pool_tokens, table, ld, _ints("ctx_len", ctx_len, B), B, M, Hq, heads, max_ctx, pre_table, pre_ld,
+            _ints("prefix_len", prefix_len, n_groups), _ints("group_start", group_start, n_groups + 1), n_groups, max_prefix,
+            softmax_scale, workspace.data_ptr(), workspace.numel() * workspace.element_size(), _stream()))
 
     @staticmethod
     def attn_prefix_paged_workspace_bytes(B, M, Hq, Hkv, max_ctx, n_groups, max_prefix):
@@ -617,18 +636,19 @@ class Context:
 
     @staticmethod
     def _paged_queries(q, out):
-        if q.dim() != 4 or q.shape[3] != D or q.shape != out.shape or not (q.is_contiguous() and out.is_contiguous()) or \
-                _dtype_code(q) != PQ_BF16 or not (q.is_cuda and out.is_cuda):
+        shape = q.shape
+        if len(shape) != 4 or shape[3] != D or shape != out.shape or _dtype_code(q) != PQ_BF16 or not (q.is_cuda and out.is_cuda) or \
+                not (q.is_contiguous() and out.is_contiguous()):
             raise PolarQuantError("q and out must be contiguous device tensors [B, M, Hq, 128], q bfloat16")
-        return int(q.shape[0]), int(q.shape[1]), int(q.shape[2])
+        return shape[0], shape[1], shape[2]
 
     @staticmethod
     def _query_positions(positions, B, M):
         if positions is None:
             return None
-        if not positions.is_contiguous():
-            raise PolarQuantError("positions must be contiguous")
-        return _ints("positions", positions, (B, M))
+        if positions.shape != (B, M) or not positions.is_contiguous():
+            raise PolarQuantError("positions must be contiguous, [B, M]")
+        return _ints("positions", positions.view(-1), B * M)
 
     @staticmethod
     def attn_paged_workspace_bytes(B, M, Hq, Hkv, max_ctx):

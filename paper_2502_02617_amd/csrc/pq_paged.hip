@@ -789,7 +789,11 @@ extern "C" pq_status pq_append_paged(const pq_ctx *ctx, const void *xk, const vo
                       pq_rotary_args(rotary), positions, ds->exact, ds->consts};
     const int64_t n_vec = n_rows * n_heads;
     hipStream_t s = static_cast<hipStream_t>(hip_stream);
-    if (n_rows >= 8 * (int64_t)n_seq) {
+    /* Whole tiles or vectors one by one: a vector takes 4.1 ns beyond the first few hundred (S, 128 KB, is fetched for every four), a tile that
+       is written in part 15 ns and one number of a tile for every sequence whether it has tokens in it or not, the first of them 6 us more
+       (heads x sequences x tokens each, us, vectors / tiles: 8 x 1 x 128 14.1 / 14.1, 512 40 / 14; 8 x 64 x 4 24 / 43, 8 39 / 43, 16 72 / 46; 8 x 256 x 1
+       25 / 71, 8 142 / 142; 8 x 16 x 16 24 / 21). */
+    if (n_rows >= 8 * (int64_t)n_seq + 768 / n_heads) {
         if (xt == PQ_BF16) launch_chunks<PQ_BF16>(ctx, ds, a, s);
         else launch_chunks<PQ_F32>(ctx, ds, a, s);
         PQ_HIP_TRY(hipGetLastError());
