@@ -1434,18 +1434,58 @@ __global__ __launch_bounds__(512) void pq_rotate_q_kernel(RotateArgs a, PlanArgs
 
 #include "pq_prefix.h"
 
-/* First launch of attention with prefixes: as above, and one more workgroup builds the plan of the groups' row blocks */
+/* First launch of attention with prefixes: as above, and one more workgroup builds the plan of the groups' row blocks and leaves the
+ * blocks and every sequence's place in them.  The plan counts pieces, not tiles: a stream of T tiles is cut into ceil(T / c) of them with the
+ * smallest c for which there is one for a workgroup at most, so that none goes on into the next stream, whose start and end would cost a
+ * workgroup another 6 us, three tiles' time (6 groups, 50 sequences: 27 -> 23 us).  With more streams than workgroups c is 1. */
 template <bool ROT>
-__global__ __launch_bounds__(512) void pq_rotate_q_prefix_kernel(RotateArgs a, PlanArgs p, PlanArgs pre, BlockRows *blocks, int rows, int row_blocks)
+__global__ __launch_bounds__(512) void pq_rotate_q_prefix_kernel(RotateArgs a, PlanArgs p, PlanArgs pre, BlockRows *blocks, SequenceRows *seqs, int rows,
+                                                                 int row_blocks)
 {
-    if ((int)blockIdx.x < row_blocks) rotate_query_rows<ROT>(a, kRotateRows * (int)blockIdx.x, rows);
-    else if ((int)blockIdx.x == row_blocks) build_plan(p);
-    else
-        build_plan(pre, [&](int i) {
-            const BlockRows r = row_block(a.groups, i, p.B, a.M * (a.Hq / p.Hkv), kPrefixRows);
+    if ((int)blockIdx.x < row_blocks) {
+        rotate_query_rows<ROT>(a, kRotateRows * (int)blockIdx.x, rows);
+    } else if ((int)blockIdx.x == row_blocks) {
+        build_plan(p);
+    } else {
+        __shared__ int sum[8];
+        const int tid = threadIdx.x, pairs = a.M * (a.Hq / p.Hkv);
+        int tiles = 0, streams = 0;
+        for (int i = tid; i < pre.B; i += 512) {
+            const BlockRows r = row_block(a.groups, i, p.B, pairs, kPrefixRows);
             blocks[i] = r;
-            return (r.tokens + 63) >> 6;
-        });
+            tiles += (r.tokens + 63) >> 6;
+            streams += r.tokens > 0;
+        }
+        for (int b = tid; b < p.B; b += 512) seqs[b] = sequence_rows(a.groups, b, pairs, kPrefixRows);
+        auto total = [&](int v) { /* of the workgroup */
+#pragma unroll
+            for (int d = 32; d >= 1; d >>= 1) v += __shfl_xor(v, d);
+            __syncthreads();
+            if ((tid & 63) == 0) sum[tid >> 6] = v;
+            __syncthreads();
+            int all = 0;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) all += sum[k];
+            return all;
+        };
+        const int all_tiles = total(tiles) * pre.Hkv, all_streams = total(streams) * pre.Hkv; /* tiles of a group's table: fewer than 2^31 in all */
+        auto pieces = [&](int c) {
+            int n = 0;
+            for (int i = tid; i < pre.B; i += 512) n += (((blocks[i].tokens + 63) >> 6) + c - 1) / c;
+            return total(n) * pre.Hkv;
+        };
+        int c = 1;
+        if (all_streams < pre.slots) { /* the smallest c with a workgroup for every piece */
+            c = max((all_tiles + pre.slots - 1) / pre.slots, 1);
+            int hi = max((all_tiles + pre.slots - all_streams - 1) / (pre.slots - all_streams), c); /* ceil(T / c) <= T / c + 1: enough */
+            while (c < hi) {
+                const int mid = (c + hi) >> 1;
+                if (pieces(mid) <= pre.slots) hi = mid;
+                else c = mid + 1;
+            }
+        }
+        build_plan(pre, [&](int i) { return (((blocks[i].tokens + 63) >> 6) + c - 1) / c; });
+    }
 }
 
 /* First launch of a whole decode step: the first workgroup builds the work plan (a chain of loads and scans, the
@@ -1496,7 +1536,7 @@ struct CombineArgs {
     const float *pre_ml, *pre_o;
     const int32_t *pre_plan;
     int pre_blocks;
-    PrefixGroups groups;
+    const SequenceRows *seq_rows;
     PqHadamard had; /* on: the un-rotation by S^T is a fast Walsh-Hadamard transform, St is not read */
 };
 
@@ -1554,10 +1594,10 @@ __global__ __launch_bounds__(512) void pq_attn_combine_kernel(CombineArgs a, int
     int used_p = 0;
     const float *pml = nullptr, *pop = nullptr;
     if (PREFIX) {
-        const int g = group_of_sequence(a.groups, __builtin_amdgcn_readfirstlane(b), tid & 63); /* 32 CQ threads of a row: whole wavefronts */
-        if (g >= 0) {
-            const int i = (b - max(a.groups.start[g], 0)) * pairs + pair;
-            const int64_t block = first_block(a.groups, g, pairs, kPrefixRows) + i / kPrefixRows, stream2 = block * a.Hkv + hk;
+        const SequenceRows sr = a.seq_rows[b];
+        if (sr.block >= 0) {
+            const int i = sr.row + pair;
+            const int64_t stream2 = (int64_t)(sr.block + i / kPrefixRows) * a.Hkv + hk;
             const int32_t *st = a.pre_plan + kPlanHeader + a.pre_blocks + 1 + 2 * stream2;
             const int64_t slot = (st[0] + stream2) * kPrefixRows + i % kPrefixRows;
             used_p = st[1];
@@ -1950,7 +1990,7 @@ struct StepPrefix {
 /* Row blocks, pieces and workspace of the prefix's part, behind `before` bytes: plan | (m, l) | o' */
 struct PrefixPlan {
     int n_blocks, slots;
-    size_t off_plan, off_blocks, off_ml, off_o, total;
+    size_t off_plan, off_blocks, off_seq, off_ml, off_o, total;
 };
 
 PrefixPlan make_prefix_plan(int B, int M, int Hq, int Hkv, int n_groups, int64_t max_prefix, size_t before)
@@ -1963,7 +2003,8 @@ PrefixPlan make_prefix_plan(int B, int M, int Hq, int Hkv, int n_groups, int64_t
     const size_t pieces = (size_t)p.slots + (size_t)p.n_blocks * Hkv;
     p.off_plan = (before + 255) & ~(size_t)255;
     p.off_blocks = (p.off_plan + (kPlanHeader + (size_t)p.n_blocks + 1 + 2 * (size_t)p.n_blocks * Hkv) * sizeof(int32_t) + 255) & ~(size_t)255;
-    p.off_ml = (p.off_blocks + (size_t)p.n_blocks * sizeof(BlockRows) + 255) & ~(size_t)255;
+    p.off_seq = (p.off_blocks + (size_t)p.n_blocks * sizeof(BlockRows) + 255) & ~(size_t)255;
+    p.off_ml = (p.off_seq + (size_t)B * sizeof(SequenceRows) + 255) & ~(size_t)255;
     p.off_o = (p.off_ml + pieces * kPrefixRows * 2 * sizeof(float) + 255) & ~(size_t)255;
     p.total = p.off_o + pieces * kPrefixRows * PQ_D * sizeof(float);
     return p;
@@ -2003,7 +2044,7 @@ void launch_combine_rows(int rows, bool hybrid, hipStream_t s, const CombineArgs
 {
     const dim3 grid((unsigned)((rows + ROWS - 1) / ROWS)), blk(512);
     if (hybrid) hipLaunchKernelGGL((pq_attn_combine_kernel<ROWS, true, false>), grid, blk, 0, s, ca, rows);
-    else if (ca.groups.n) hipLaunchKernelGGL((pq_attn_combine_kernel<ROWS, false, true>), grid, blk, 0, s, ca, rows);
+    else if (ca.seq_rows) hipLaunchKernelGGL((pq_attn_combine_kernel<ROWS, false, true>), grid, blk, 0, s, ca, rows);
     else hipLaunchKernelGGL((pq_attn_combine_kernel<ROWS, false, false>), grid, blk, 0, s, ca, rows);
 }
 
@@ -2091,6 +2132,7 @@ pq_status attention_launches(const pq_ctx *ctx, const StepAppend *app, const Ste
                   pre ? PrefixGroups{pre->group_start, pre->len, pre->n_groups, pre->max_len} : PrefixGroups{}, M, Hq};
     int32_t *pre_plan = reinterpret_cast<int32_t *>(ws + pp.off_plan);
     BlockRows *pre_blocks = reinterpret_cast<BlockRows *>(ws + pp.off_blocks);
+    SequenceRows *seq_rows = reinterpret_cast<SequenceRows *>(ws + pp.off_seq);
     if (app) {
         AppendArgs ak{app->xk, k_codes, k_radii, pool_tokens / 64, pool_tokens, app->dst_token, Hkv, ds->S_f32, ds->consts, ctx->hadamard};
         AppendArgs av{app->xv, v_codes, v_radii, pool_tokens / 64, pool_tokens, app->dst_token, Hkv, ds->S_f32, ds->consts, ctx->hadamard};
@@ -2114,7 +2156,7 @@ pq_status attention_launches(const pq_ctx *ctx, const StepAppend *app, const Ste
         else hipLaunchKernelGGL(pq_rotate_window_kernel<1>, grid, blk, 0, s, ra, pa, rows, row_blocks, wa, (int)wblocks);
     } else if (pre) {
         const PlanArgs pb{nullptr, nullptr, pp.n_blocks, Hkv, 0, 0, pp.slots, pre_plan};
-        auto rotate = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((unsigned)row_blocks + 2u), dim3(512), 0, s, ra, pa, pb, pre_blocks, rows, row_blocks); };
+        auto rotate = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((unsigned)row_blocks + 2u), dim3(512), 0, s, ra, pa, pb, pre_blocks, seq_rows, rows, row_blocks); };
         if (ra.rot.cs) rotate(pq_rotate_q_prefix_kernel<true>);
         else rotate(pq_rotate_q_prefix_kernel<false>);
     } else {
@@ -2158,7 +2200,7 @@ pq_status attention_launches(const pq_ctx *ctx, const StepAppend *app, const Ste
                    reinterpret_cast<const float *>(ws + p.off_wml), reinterpret_cast<const float *>(ws + p.off_wo),
                    win ? win->win_len : nullptr, p.n_wchunks, win ? (int)win->win_cap : 0,
                    reinterpret_cast<const float *>(ws + pp.off_ml), reinterpret_cast<const float *>(ws + pp.off_o), pre_plan, pp.n_blocks,
-                   ra.groups, ctx->hadamard};
+                   pre ? seq_rows : nullptr, ctx->hadamard};
     launch_combine(rows, win != nullptr, s, ca);
     PQ_HIP_TRY(hipGetLastError());
     return PQ_OK;

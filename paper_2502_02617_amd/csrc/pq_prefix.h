@@ -35,7 +35,7 @@ struct PrefixArgs {
     PagedTable table; /* one row per group */
     PrefixGroups groups;
     int B, Hq, Hkv, M;
-    const int32_t *plan; /* as the other kernel's, of row blocks instead of sequences */
+    const int32_t *plan; /* as the other kernel's, of row blocks instead of sequences and their pieces instead of tiles */
     const BlockRows *blocks;
     int n_blocks;        /* row blocks that the plan counts */
     float *ws_ml; /* [piece][ROWS][2] */
@@ -71,6 +71,24 @@ __device__ __forceinline__ BlockRows row_block(const PrefixGroups &g, int block,
     r.seq0 = s0;
     r.tokens = prefix_length(g, i);
     return r;
+}
+
+/* A sequence's rows in its group's blocks: the block that the group begins with (-1: no group) and the sequence's first row in the group. */
+struct SequenceRows {
+    int block, row;
+};
+
+__device__ __forceinline__ SequenceRows sequence_rows(const PrefixGroups &g, int b, int pairs, int rows)
+{
+    int lo = 0, hi = g.n; /* the last group that begins with the sequence or ahead of it */
+    while (lo <= hi) {
+        const int mid = (lo + hi) >> 1;
+        if (g.start[mid] <= b) lo = mid + 1;
+        else hi = mid - 1;
+    }
+    const int i = lo - 1;
+    if (i < 0 || i >= g.n) return SequenceRows{-1, 0};
+    return SequenceRows{(int)first_block(g, i, pairs, rows), (b - max(g.start[i], 0)) * pairs};
 }
 
 /* Row `i` of a group -> row of q: (sequence, query token, head of the kv head's group) */
@@ -248,13 +266,13 @@ __global__ __launch_bounds__(kPrefixThreads, 1) void pq_attn_prefix_kernel(Prefi
     int blk = few ? __popcll(__ballot(lane <= a.n_blocks && (int64_t)pre * a.Hkv <= gpos)) - 1
                   : paged_find(a.n_blocks, gpos, lane, [&](int i) { return (int64_t)a.plan[kPlanHeader + i] * a.Hkv; });
     blk = min(max(blk, 0), a.n_blocks - 1);
-    int before = prefix_at(blk), block_tiles = prefix_at(blk + 1) - before;
-    if (block_tiles <= 0) return; /* cannot happen with a consistent plan */
-    int hk, tile_lo;
+    int before = prefix_at(blk), block_pieces = prefix_at(blk + 1) - before;
+    if (block_pieces <= 0) return; /* cannot happen with a consistent plan */
+    int hk, unit; /* piece of the stream */
     {
         const int r = gpos - before * a.Hkv;
-        hk = min(r / block_tiles, a.Hkv - 1);
-        tile_lo = r - hk * block_tiles;
+        hk = min(r / block_pieces, a.Hkv - 1);
+        unit = r - hk * block_pieces;
     }
     RebuildPlaces places;
     places.set(wave, lane);
@@ -264,9 +282,9 @@ __global__ __launch_bounds__(kPrefixThreads, 1) void pq_attn_prefix_kernel(Prefi
 
     for (;;) { /* one piece per round */
         const BlockRows rb = rows_of(blk);
-        const int tile_hi = min((rb.tokens + 63) >> 6, tile_lo + (gend - gpos));
-        const int piece_tiles = tile_hi - tile_lo;
-        if (piece_tiles <= 0) return; /* cannot happen with a consistent plan */
+        const int units = min(block_pieces - unit, gend - gpos), tiles = (rb.tokens + 63) >> 6, c = (tiles + block_pieces - 1) / block_pieces;
+        const int tile_lo = unit * c, tile_hi = min(tiles, tile_lo + units * c); /* ceil(tiles / c) is block_pieces again: none is empty */
+        if (tile_lo >= tile_hi) return; /* cannot happen with a consistent plan */
         const int64_t piece = (int64_t)w + (int64_t)blk * a.Hkv + hk;
         /* keys by wavefront 0, values by wavefront 1 (wavefronts of two SIMDs); a tile without a page is passed over */
         int page_base = tile_lo; /* the table's entries of 64 tiles lie in a register, one per lane */
@@ -437,16 +455,16 @@ __global__ __launch_bounds__(kPrefixThreads, 1) void pq_attn_prefix_kernel(Prefi
         }
         if (slice == 0 && real && H == 0) *reinterpret_cast<float2 *>(a.ws_ml + out_row * 2) = make_float2(m, l);
 
-        gpos += piece_tiles;
+        gpos += units;
         if (gpos >= gend) return;
-        tile_lo = 0;
+        unit = 0;
         if (++hk == a.Hkv) {
             hk = 0;
             do {
                 if (++blk >= a.n_blocks) return;
                 before = prefix_at(blk);
-                block_tiles = prefix_at(blk + 1) - before;
-            } while (block_tiles <= 0);
+                block_pieces = prefix_at(blk + 1) - before;
+            } while (block_pieces <= 0);
         }
     }
 }
