@@ -1440,7 +1440,7 @@ __global__ __launch_bounds__(512) void pq_rotate_q_kernel(RotateArgs a, PlanArgs
  * workgroup another 6 us, three tiles' time (6 groups, 50 sequences: 27 -> 23 us).  With more streams than workgroups c is 1. */
 template <bool ROT>
 __global__ __launch_bounds__(512) void pq_rotate_q_prefix_kernel(RotateArgs a, PlanArgs p, PlanArgs pre, BlockRows *blocks, SequenceRows *seqs, int rows,
-                                                                 int row_blocks)
+                                                                 int row_blocks, int pre_rows)
 {
     if ((int)blockIdx.x < row_blocks) {
         rotate_query_rows<ROT>(a, kRotateRows * (int)blockIdx.x, rows);
@@ -1451,12 +1451,12 @@ __global__ __launch_bounds__(512) void pq_rotate_q_prefix_kernel(RotateArgs a, P
         const int tid = threadIdx.x, pairs = a.M * (a.Hq / p.Hkv);
         int tiles = 0, streams = 0;
         for (int i = tid; i < pre.B; i += 512) {
-            const BlockRows r = row_block(a.groups, i, p.B, pairs, kPrefixRows);
+            const BlockRows r = row_block(a.groups, i, p.B, pairs, pre_rows);
             blocks[i] = r;
             tiles += (r.tokens + 63) >> 6;
             streams += r.tokens > 0;
         }
-        for (int b = tid; b < p.B; b += 512) seqs[b] = sequence_rows(a.groups, b, pairs, kPrefixRows);
+        for (int b = tid; b < p.B; b += 512) seqs[b] = sequence_rows(a.groups, b, pairs, pre_rows);
         auto total = [&](int v) { /* of the workgroup */
 #pragma unroll
             for (int d = 32; d >= 1; d >>= 1) v += __shfl_xor(v, d);
@@ -1532,10 +1532,10 @@ struct CombineArgs {
     const float *win_ml, *win_o;
     const int32_t *win_len;
     int n_wchunks, win_cap;
-    /* common prefixes (PREFIX): partial results of row blocks, (m, l) [piece][kPrefixRows][2] and o' likewise, and their plan */
+    /* common prefixes (PREFIX): partial results of row blocks, (m, l) [piece][pre_rows][2] and o' likewise, and their plan */
     const float *pre_ml, *pre_o;
     const int32_t *pre_plan;
-    int pre_blocks;
+    int pre_blocks, pre_rows;
     const SequenceRows *seq_rows;
     PqHadamard had; /* on: the un-rotation by S^T is a fast Walsh-Hadamard transform, St is not read */
 };
@@ -1597,9 +1597,9 @@ __global__ __launch_bounds__(512) void pq_attn_combine_kernel(CombineArgs a, int
         const SequenceRows sr = a.seq_rows[b];
         if (sr.block >= 0) {
             const int i = sr.row + pair;
-            const int64_t stream2 = (int64_t)(sr.block + i / kPrefixRows) * a.Hkv + hk;
+            const int64_t stream2 = (int64_t)(sr.block + i / a.pre_rows) * a.Hkv + hk;
             const int32_t *st = a.pre_plan + kPlanHeader + a.pre_blocks + 1 + 2 * stream2;
-            const int64_t slot = (st[0] + stream2) * kPrefixRows + i % kPrefixRows;
+            const int64_t slot = (st[0] + stream2) * a.pre_rows + i % a.pre_rows;
             used_p = st[1];
             pml = a.pre_ml + slot * 2;
             pop = a.pre_o + slot * PQ_D + col;
@@ -1613,7 +1613,7 @@ __global__ __launch_bounds__(512) void pq_attn_combine_kernel(CombineArgs a, int
         if (HYBRID)
             for (int c = lane; c < used_w; c += 32) m = fmaxf(m, wml[2 * c]);
         if (PREFIX)
-            for (int c = lane; c < used_p; c += 32) m = fmaxf(m, pml[(int64_t)c * (2 * kPrefixRows)]);
+            for (int c = lane; c < used_p; c += 32) m = fmaxf(m, pml[(int64_t)c * (2 * a.pre_rows)]);
 #pragma unroll
         for (int d = 16; d >= 1; d >>= 1) m = fmaxf(m, __shfl_xor(m, d));
     }
@@ -1632,8 +1632,8 @@ __global__ __launch_bounds__(512) void pq_attn_combine_kernel(CombineArgs a, int
         if (PREFIX) {
 #pragma unroll 4
             for (int c = cq; c < used_p; c += CQ)
-                add(*reinterpret_cast<const float2 *>(pml + (int64_t)c * (2 * kPrefixRows)),
-                    *reinterpret_cast<const float4 *>(pop + (int64_t)c * (PQ_D * kPrefixRows)));
+                add(*reinterpret_cast<const float2 *>(pml + (int64_t)c * (2 * a.pre_rows)),
+                    *reinterpret_cast<const float4 *>(pop + (int64_t)c * (PQ_D * a.pre_rows)));
         }
     }
     if (HYBRID) {
@@ -1989,7 +1989,7 @@ struct StepPrefix {
 
 /* Row blocks, pieces and workspace of the prefix's part, behind `before` bytes: plan | (m, l) | o' */
 struct PrefixPlan {
-    int n_blocks, slots;
+    int rows, n_blocks, slots; /* rows: of a block */
     size_t off_plan, off_blocks, off_seq, off_ml, off_o, total;
 };
 
@@ -1997,7 +1997,11 @@ PrefixPlan make_prefix_plan(int B, int M, int Hq, int Hkv, int n_groups, int64_t
 {
     PrefixPlan p;
     const int pairs = M * (Hq / Hkv);
-    p.n_blocks = (int)((int64_t)B * pairs / kPrefixRows) + n_groups; /* first_block of the end */
+    /* blocks of 256 rows rebuild a tile half as often: 160 rows x 16384 tokens 58 us, 67 in blocks of 128; but where a group has no more than
+     * 128 of them half of each tile's products were for nothing, and a row's partial results come from twice as many workgroups (256 rows x 4096
+     * tokens 50 and 49 us).  Only the average is known here. */
+    p.rows = (int64_t)B * pairs > 128 * (int64_t)n_groups ? 256 : 128;
+    p.n_blocks = (int)((int64_t)B * pairs / p.rows) + n_groups; /* first_block of the end */
     const int64_t tiles = max_prefix <= 0 ? 0 : (max_prefix + 63) / 64, most = (int64_t)p.n_blocks * Hkv * tiles;
     p.slots = (int)(most < 256 ? (most < 1 ? 1 : most) : 256); /* one workgroup per CU */
     const size_t pieces = (size_t)p.slots + (size_t)p.n_blocks * Hkv;
@@ -2005,8 +2009,8 @@ PrefixPlan make_prefix_plan(int B, int M, int Hq, int Hkv, int n_groups, int64_t
     p.off_blocks = (p.off_plan + (kPlanHeader + (size_t)p.n_blocks + 1 + 2 * (size_t)p.n_blocks * Hkv) * sizeof(int32_t) + 255) & ~(size_t)255;
     p.off_seq = (p.off_blocks + (size_t)p.n_blocks * sizeof(BlockRows) + 255) & ~(size_t)255;
     p.off_ml = (p.off_seq + (size_t)B * sizeof(SequenceRows) + 255) & ~(size_t)255;
-    p.off_o = (p.off_ml + pieces * kPrefixRows * 2 * sizeof(float) + 255) & ~(size_t)255;
-    p.total = p.off_o + pieces * kPrefixRows * PQ_D * sizeof(float);
+    p.off_o = (p.off_ml + pieces * p.rows * 2 * sizeof(float) + 255) & ~(size_t)255;
+    p.total = p.off_o + pieces * p.rows * PQ_D * sizeof(float);
     return p;
 }
 
@@ -2111,7 +2115,7 @@ pq_status attention_launches(const pq_ctx *ctx, const StepAppend *app, const Ste
     PrefixPlan pp{};
     if (pre) { /* the same limits for the row blocks' tiles as for the sequences' */
         pp = make_prefix_plan(B, M, Hq, Hkv, pre->n_groups, pre->max_len, p.total);
-        if (((int64_t)B * M * G / kPrefixRows + pre->n_groups) * Hkv * ((pre->max_len + 63) / 64) >= ((int64_t)1 << 31) - 4096) return PQ_EUNSUPPORTED;
+        if (((int64_t)B * M * G / 128 + pre->n_groups) * Hkv * ((pre->max_len + 63) / 64) >= ((int64_t)1 << 31) - 4096) return PQ_EUNSUPPORTED;
     }
     if (workspace_bytes < (pre ? pp.total : p.total)) return PQ_ENOMEM;
     const PqDeviceState *ds = nullptr;
@@ -2156,7 +2160,7 @@ pq_status attention_launches(const pq_ctx *ctx, const StepAppend *app, const Ste
         else hipLaunchKernelGGL(pq_rotate_window_kernel<1>, grid, blk, 0, s, ra, pa, rows, row_blocks, wa, (int)wblocks);
     } else if (pre) {
         const PlanArgs pb{nullptr, nullptr, pp.n_blocks, Hkv, 0, 0, pp.slots, pre_plan};
-        auto rotate = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((unsigned)row_blocks + 2u), dim3(512), 0, s, ra, pa, pb, pre_blocks, seq_rows, rows, row_blocks); };
+        auto rotate = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((unsigned)row_blocks + 2u), dim3(512), 0, s, ra, pa, pb, pre_blocks, seq_rows, rows, row_blocks, pp.rows); };
         if (ra.rot.cs) rotate(pq_rotate_q_prefix_kernel<true>);
         else rotate(pq_rotate_q_prefix_kernel<false>);
     } else {
@@ -2190,8 +2194,12 @@ pq_status attention_launches(const pq_ctx *ctx, const StepAppend *app, const Ste
                             PagedTable{pre->pages, pre->ld_pages, pool_tokens / 64}, ra.groups, B, Hq, Hkv, M, pre_plan, pre_blocks, pp.n_blocks,
                             reinterpret_cast<float *>(ws + pp.off_ml), reinterpret_cast<float *>(ws + pp.off_o), ds->consts};
         auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((unsigned)pp.slots), dim3(kPrefixThreads), 0, s, xa); };
-        if (ctx->depth == 7) launch(pq_attn_prefix_kernel<true>);
-        else launch(pq_attn_prefix_kernel<false>);
+        auto depth = [&](auto rows) {
+            if (ctx->depth == 7) launch(pq_attn_prefix_kernel<true, decltype(rows)::value>);
+            else launch(pq_attn_prefix_kernel<false, decltype(rows)::value>);
+        };
+        if (pp.rows == 256) depth(std::integral_constant<int, 256>{});
+        else depth(std::integral_constant<int, 128>{});
     }
     pq_prof_after(0, s);
 
@@ -2199,7 +2207,7 @@ pq_status attention_launches(const pq_ctx *ctx, const StepAppend *app, const Ste
                    ds->St_f32, out, out_dtype == PQ_F32 ? 1 : 0, ds->consts,
                    reinterpret_cast<const float *>(ws + p.off_wml), reinterpret_cast<const float *>(ws + p.off_wo),
                    win ? win->win_len : nullptr, p.n_wchunks, win ? (int)win->win_cap : 0,
-                   reinterpret_cast<const float *>(ws + pp.off_ml), reinterpret_cast<const float *>(ws + pp.off_o), pre_plan, pp.n_blocks,
+                   reinterpret_cast<const float *>(ws + pp.off_ml), reinterpret_cast<const float *>(ws + pp.off_o), pre_plan, pp.n_blocks, pp.rows,
                    pre ? seq_rows : nullptr, ctx->hadamard};
     launch_combine(rows, win != nullptr, s, ca);
     PQ_HIP_TRY(hipGetLastError());

@@ -19,7 +19,7 @@
 
 typedef float f16x __attribute__((ext_vector_type(16)));
 
-constexpr int kPrefixThreads = 512, kPrefixRows = 128;
+constexpr int kPrefixThreads = 512;
 
 /* A block of query rows, as the launch that builds the plan leaves it for this one: rows first .. first + rows - 1 of the group that begins with
  * sequence seq0, and the tokens of its prefix. */
@@ -38,7 +38,7 @@ struct PrefixArgs {
     const int32_t *plan; /* as the other kernel's, of row blocks instead of sequences and their pieces instead of tiles */
     const BlockRows *blocks;
     int n_blocks;        /* row blocks that the plan counts */
-    float *ws_ml; /* [piece][ROWS][2] */
+    float *ws_ml; /* [piece][ROWS][2], ROWS query rows in a block */
     float *ws_o;  /* [piece][ROWS][128] */
     const PqDeviceConsts *consts;
 };
@@ -222,13 +222,15 @@ struct Rebuild {
     }
 };
 
-/* kPrefixRows rows per workgroup, 32 per wavefront; two wavefronts share rows and have half of a tile's tokens each.  While a tile is
- * multiplied the next one is rebuilt into the other half of LDS, and the one after that is on its way there: one barrier per tile.  What
- * bounds it is the chain of a wavefront's steps, two wavefronts per SIMD: so all requests to LDS stand ahead of the work that covers them. */
-template <bool DEEP>
+/* ROWS query rows per workgroup, 32 per wavefront: of 256 a wavefront sees all tokens of a tile, of 128 two wavefronts share rows and have
+ * half of the tokens each, and join their results in the end.  While a tile is multiplied the next one is rebuilt into the other half of LDS,
+ * and the one after that is on its way there: one barrier per tile.  What bounds it is the chain of a wavefront's steps, two wavefronts per
+ * SIMD: so all requests to LDS stand ahead of the work that covers them. */
+template <bool DEEP, int ROWS>
 __global__ __launch_bounds__(kPrefixThreads, 1) void pq_attn_prefix_kernel(PrefixArgs a)
 {
-    static_assert(kPrefixRows == 128 && kPrefixThreads == 512, "four row groups, two slices of 32 tokens");
+    static_assert((ROWS == 128 || ROWS == 256) && kPrefixThreads == 512, "row groups of 32 by eight wavefronts");
+    constexpr int kSlices = ROWS / 128; /* of 32 tokens, that a wavefront multiplies */
     __shared__ PrefixTables tab;
     __shared__ RawTile sRaw[2][2];                                 /* [buffer][keys, values] */
     __shared__ __attribute__((aligned(16))) uint4 sK[2][64 * 16];  /* [token][chunk of eight coordinates ^ token & 15] */
@@ -278,7 +280,7 @@ __global__ __launch_bounds__(kPrefixThreads, 1) void pq_attn_prefix_kernel(Prefi
     places.set(wave, lane);
     const int G = a.Hq / a.Hkv;
     constexpr int kRadiiHalves = DEEP ? PQ_DEEP_RADII_HALVES : PQL_RADII;
-    const int rg = (wave >> 1) & 3, slice = wave & 1, H = lane >> 5, r32 = lane & 31;
+    const int rg = kSlices == 1 ? wave >> 1 : wave, slice = kSlices == 1 ? wave & 1 : 0, H = lane >> 5, r32 = lane & 31;
 
     for (;;) { /* one piece per round */
         const BlockRows rb = rows_of(blk);
@@ -328,9 +330,7 @@ __global__ __launch_bounds__(kPrefixThreads, 1) void pq_attn_prefix_kernel(Prefi
 #pragma unroll
             for (int e = 0; e < 16; ++e) acc[d][e] = 0.f;
         float m_ref = 0.f, l_run = 0.f;
-        f16x start; /* what a tile's scores begin with */
-#pragma unroll
-        for (int e = 0; e < 16; ++e) start[e] = kProbShift;
+        float start = kProbShift; /* what a tile's scores begin with */
         bool have_ref = false;
         /* tokens of tile t that are looked at: a tile without a page has none */
         auto tokens_of = [&](int t, int p) { return p < 0 ? 0 : min(rb.tokens - 64 * t, 64); };
@@ -355,29 +355,41 @@ __global__ __launch_bounds__(kPrefixThreads, 1) void pq_attn_prefix_kernel(Prefi
             const int lH = l >> 5, lr = l & 31, tok = 32 * slice + lr;
             Rebuild<DEEP> r;
             r.fetch(sRaw[nxt][0], sRaw[nxt][1], places, wave, l);
+            auto key = [&](int ks, int sl) { return sK[cur][16 * (tok + 32 * sl) + ((2 * ks + lH) ^ (tok & 15))]; };
+            auto value = [&](int d, int k, int sl) { return sV[cur][value_place(32 * d + lr, 2 * (2 * (slice + sl) + k) + lH)]; };
             H8 ko[8];
 #pragma unroll
-            for (int ks = 0; ks < 8; ++ks) ko[ks].q = sK[cur][16 * tok + ((2 * ks + lH) ^ (tok & 15))];
-            __builtin_amdgcn_sched_barrier(0);
+            for (int ks = 0; ks < 8; ++ks) ko[ks].q = key(ks, 0);
             r.gather(a, tab, sRaw[nxt][1].w, wave, nv1, l);
-            f16x s = start;
+            f16x s[kSlices];
 #pragma unroll
-            for (int ks = 0; ks < 8; ++ks) s = __builtin_amdgcn_mfma_f32_32x32x16_f16(ko[ks].v, q[ks], s, 0, 0, 0);
-            __builtin_amdgcn_sched_barrier(0);
+            for (int sl = 0; sl < kSlices; ++sl) {
+#pragma unroll
+                for (int e = 0; e < 16; ++e) s[sl][e] = start;
+#pragma unroll
+                for (int ks = 0; ks < 8; ++ks) {
+                    s[sl] = __builtin_amdgcn_mfma_f32_32x32x16_f16(ko[ks].v, q[ks], s[sl], 0, 0, 0);
+                    if (sl + 1 < kSlices) ko[ks].q = key(ks, sl + 1);
+                }
+            }
             H8 vo[8];
 #pragma unroll
             for (int d = 0; d < 4; ++d)
 #pragma unroll
-                for (int k = 0; k < 2; ++k) vo[2 * d + k].q = sV[cur][value_place(32 * d + lr, 2 * (2 * slice + k) + lH)];
+                for (int k = 0; k < 2; ++k) vo[2 * d + k].q = value(d, k, 0);
             if (nv < 64) {
 #pragma unroll
-                for (int e = 0; e < 16; ++e)
-                    if (32 * slice + 8 * (e >> 2) + 4 * lH + (e & 3) >= nv) s[e] = -INFINITY;
-            }
-            float top = s[0];
+                for (int sl = 0; sl < kSlices; ++sl)
 #pragma unroll
-            for (int e = 1; e < 16; ++e) top = fmaxf(top, s[e]);
-            /* the first tokens that this slice sees set the reference of its rows */
+                    for (int e = 0; e < 16; ++e)
+                        if (32 * (slice + sl) + 8 * (e >> 2) + 4 * lH + (e & 3) >= nv) s[sl][e] = -INFINITY;
+            }
+            float top = s[0][0];
+#pragma unroll
+            for (int sl = 0; sl < kSlices; ++sl)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) top = fmaxf(top, s[sl][e]);
+            /* the first tokens that this wavefront sees set the reference of its rows */
             if (nv > 32 * slice && (!have_ref || __ballot(top > kProbShift + kRefSlack) != 0ull)) {
                 top = fmaxf(top, __shfl_xor(top, 32));
                 float delta = top == -INFINITY ? 0.f : top - kProbShift;
@@ -385,73 +397,89 @@ __global__ __launch_bounds__(kPrefixThreads, 1) void pq_attn_prefix_kernel(Prefi
                 const float alpha = have_ref ? __builtin_amdgcn_exp2f(-delta) : 1.f;
                 m_ref += delta;
                 l_run *= alpha;
+                start = kProbShift - m_ref;
 #pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                    s[e] -= delta;
-                    start[e] = kProbShift - m_ref;
-                }
+                for (int sl = 0; sl < kSlices; ++sl) s[sl] -= delta;
 #pragma unroll
                 for (int d = 0; d < 4; ++d) acc[d] *= alpha;
                 have_ref = true;
             }
-            H8 p[2];
 #pragma unroll
-            for (int e = 0; e < 16; e += 2) {
-                const float x = __builtin_amdgcn_exp2f(s[e]), y = __builtin_amdgcn_exp2f(s[e + 1]);
-                l_run += x + y;
-                p[e >> 3].p[(e & 7) >> 1] = h2{(_Float16)x, (_Float16)y};
+            for (int sl = 0; sl < kSlices; ++sl) {
+                H8 p[2];
+#pragma unroll
+                for (int e = 0; e < 16; e += 2) {
+                    const float x = __builtin_amdgcn_exp2f(s[sl][e]), y = __builtin_amdgcn_exp2f(s[sl][e + 1]);
+                    l_run += x + y;
+                    p[e >> 3].p[(e & 7) >> 1] = h2{(_Float16)x, (_Float16)y};
+                }
+#pragma unroll
+                for (int k = 0; k < 2; ++k)
+#pragma unroll
+                    for (int d = 0; d < 4; ++d) {
+                        acc[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vo[2 * d + k].v, p[k].v, acc[d], 0, 0, 0);
+                        if (sl + 1 < kSlices) vo[2 * d + k].q = value(d, k, sl + 1);
+                    }
             }
-#pragma unroll
-            for (int k = 0; k < 2; ++k)
-#pragma unroll
-                for (int d = 0; d < 4; ++d) acc[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vo[2 * d + k].v, p[k].v, acc[d], 0, 0, 0);
             r.store(sK[nxt], sV[nxt], wave, l);
             page = page1;
             page1 = page2;
         }
-        /* ---- the slices' results joined (through LDS, half of the coordinates at a time), and stored ---- */
         float l = l_run + __shfl_xor(l_run, 32), m = l > 0.f ? m_ref : -INFINITY;
-        __syncthreads();
-        if (slice == 1 && H == 0) {
-            sM[rg][r32][0] = m;
-            sM[rg][r32][1] = l;
-        }
-        float4 *theirs = reinterpret_cast<float4 *>(&sK[0][0]) + rg * 512 + lane; /* eight of 64 lanes each */
-        const int64_t out_row = piece * kPrefixRows + 32 * rg + r32;
-        float scale0 = 0.f, scale1 = 0.f;
+        const int64_t out_row = piece * ROWS + 32 * rg + r32;
+        if (kSlices == 2) {
+            if (real) {
 #pragma unroll
-        for (int half = 0; half < 2; ++half) {
-            if (slice == 1) {
-#pragma unroll
-                for (int k = 0; k < 8; ++k) {
-                    const f16x &o = acc[2 * half + (k >> 2)];
-                    theirs[64 * k] = make_float4(o[4 * (k & 3)], o[4 * (k & 3) + 1], o[4 * (k & 3) + 2], o[4 * (k & 3) + 3]);
+                for (int k = 0; k < 16; ++k) {
+                    const f16x &o = acc[k >> 2];
+                    const int j = 4 * (k & 3);
+                    *reinterpret_cast<float4 *>(a.ws_o + out_row * PQ_D + 8 * k + 4 * H) = make_float4(o[j], o[j + 1], o[j + 2], o[j + 3]);
                 }
             }
+            __syncthreads(); /* nobody reads this piece's last tile any more */
+        } else {
+            /* the slices' results joined (through LDS, half of the coordinates at a time), and stored */
             __syncthreads();
-            if (slice == 0) {
-                if (half == 0) {
-                    const float m1 = sM[rg][r32][0], l1 = sM[rg][r32][1], mm = fmaxf(m, m1);
-                    if (mm != -INFINITY) {
-                        scale0 = __builtin_amdgcn_exp2f(m - mm);
-                        scale1 = __builtin_amdgcn_exp2f(m1 - mm);
-                    }
-                    l = l * scale0 + l1 * scale1;
-                    m = mm;
-                }
-                if (real) {
+            if (slice == 1 && H == 0) {
+                sM[rg][r32][0] = m;
+                sM[rg][r32][1] = l;
+            }
+            float4 *theirs = reinterpret_cast<float4 *>(&sK[0][0]) + rg * 512 + lane; /* eight of 64 lanes each */
+            float scale0 = 0.f, scale1 = 0.f;
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+                if (slice == 1) {
 #pragma unroll
                     for (int k = 0; k < 8; ++k) {
                         const f16x &o = acc[2 * half + (k >> 2)];
-                        const float4 t = theirs[64 * k];
-                        const int j = k & 3;
-                        const float4 sum = make_float4(o[4 * j] * scale0 + t.x * scale1, o[4 * j + 1] * scale0 + t.y * scale1,
-                                                       o[4 * j + 2] * scale0 + t.z * scale1, o[4 * j + 3] * scale0 + t.w * scale1);
-                        *reinterpret_cast<float4 *>(a.ws_o + out_row * PQ_D + 32 * (2 * half + (k >> 2)) + 8 * j + 4 * H) = sum;
+                        theirs[64 * k] = make_float4(o[4 * (k & 3)], o[4 * (k & 3) + 1], o[4 * (k & 3) + 2], o[4 * (k & 3) + 3]);
                     }
                 }
+                __syncthreads();
+                if (slice == 0) {
+                    if (half == 0) {
+                        const float m1 = sM[rg][r32][0], l1 = sM[rg][r32][1], mm = fmaxf(m, m1);
+                        if (mm != -INFINITY) {
+                            scale0 = __builtin_amdgcn_exp2f(m - mm);
+                            scale1 = __builtin_amdgcn_exp2f(m1 - mm);
+                        }
+                        l = l * scale0 + l1 * scale1;
+                        m = mm;
+                    }
+                    if (real) {
+#pragma unroll
+                        for (int k = 0; k < 8; ++k) {
+                            const f16x &o = acc[2 * half + (k >> 2)];
+                            const float4 t = theirs[64 * k];
+                            const int j = k & 3;
+                            const float4 sum = make_float4(o[4 * j] * scale0 + t.x * scale1, o[4 * j + 1] * scale0 + t.y * scale1,
+                                                           o[4 * j + 2] * scale0 + t.z * scale1, o[4 * j + 3] * scale0 + t.w * scale1);
+                            *reinterpret_cast<float4 *>(a.ws_o + out_row * PQ_D + 32 * (2 * half + (k >> 2)) + 8 * j + 4 * H) = sum;
+                        }
+                    }
+                }
+                __syncthreads();
             }
-            __syncthreads();
         }
         if (slice == 0 && real && H == 0) *reinterpret_cast<float2 *>(a.ws_ml + out_row * 2) = make_float2(m, l);
 
