@@ -443,7 +443,8 @@ typedef struct pq_rotary {
  * in its sequence.  A row whose page is none is not written.
  * Codes are settled in 64 bits: a vector gets the codes of its definition -- products
  * with S, rotation and cell comparisons in double precision where fewer bits leave
- * them in doubt -- whatever batch it comes in (radii are within one rounding).
+ * them in doubt -- whatever batch it comes in (radii are within one rounding).  An angle
+ * that lies on a cell border to within double precision has the code of either side.
  * Slots of a page that the call does not name keep their contents; two calls, or two
  * sequences of one call, that write into one page must not overlap in time.
  * n_rows * n_heads at most 2^30 - 1 (PQ_EUNSUPPORTED).  n_rows == 0 or n_seq == 0 is a

@@ -1,12 +1,12 @@
 """GPU tests of attention with common prefixes (pq_attn_prefix_paged) against attention in 64 bits over prefix and own tokens.
-Tolerance: 2e-3 as for the other calls; the keys' rounding to binary16, 2^-11 of an element, is one more of the size of the query's."""
+Tolerance: 2e-3 as for the other calls; keys and values are rebuilt by binary16 products, two more roundings of 2^-11 of an element."""
 import numpy as np
 import pytest
 import torch
 
 from paper_2502_02617_amd import Context, Rotary
 from tests import helpers, paged_ref
-from tests.test_gpu_paged import DEV, check_rows, dev32, f64, filled, fmt, say
+from tests.test_gpu_paged import DEV, check_rows, dev32, f64, filled, fmt, rows, say
 
 pytestmark = pytest.mark.gpu
 
@@ -112,8 +112,9 @@ def test_a_prefix_without_any_page_and_no_tokens():
 
 @pytest.mark.parametrize("size", [1e-3, 30.0])
 def test_small_and_large_keys(size):
-    """Scores of a thousandth and of thirty times the usual size.  Two roundings to binary16 of rms 2e-4 in each of a score's 128 products leave 2.8e-4
-    of its rms: nothing at a thousandth, 0.85 % of the weights' exponent at 30 (scores of rms 30); 2e-2 is 2.4 times that."""
+    """Scores of a thousandth and of thirty times the usual size.  Roundings to binary16 have an rms of 2e-4: four of them in each of a score's 128 products
+    (query, the key's two products and its table's entry) leave 4e-4 of its rms: nothing at a thousandth, 1.2 % of the weights' exponent at 30 (scores of
+    rms 30), below 2e-2."""
     f = fmt("general")
     batch = Batch(f, 7, [20], [500], [10] * 20, 1)
     q = (queries(20, 1, 8, 7).float() * size).to(torch.bfloat16)
@@ -189,3 +190,79 @@ def test_captured_with_lengths_that_grow():
         call(eager)
         torch.cuda.synchronize()
         assert torch.equal(eager, out)
+
+
+@pytest.mark.parametrize("shape", [(80, 2, 8, 4, 140), (70, 9, 64, 4, 70)])
+def test_more_row_blocks_than_lanes_and_more_streams_than_workgroups(shape):
+    """Groups x kv heads above 256: a workgroup goes on from one stream into the next; blocks of 128 rows, and of 256."""
+    groups, each, Hq, Hkv, longest = shape
+    f, rng = fmt("general"), np.random.default_rng(21)
+    prefix = [int(n) for n in rng.integers(0, longest, size=groups)]
+    sizes = [int(n) for n in rng.integers(0, each + 1, size=groups)] if each < 3 else [each] * groups
+    own = [int(n) for n in rng.integers(0, 20, size=sum(sizes) + 2)]
+    batch = Batch(f, 21, sizes, prefix, own, Hkv, ahead=1)
+    q = queries(len(own), 1, Hq, 21)
+    check_rows(f64(batch.run(q)), batch.want(f64(q)), batch.total())
+
+
+def test_two_calls_at_once():
+    """Two streams, two workspaces: the results of calls one after the other."""
+    f = fmt("general")
+    batches = [Batch(f, 30 + i, [20], [3000 + 500 * i], [40] * 20, 2) for i in range(2)]
+    q = [queries(20, 1, 8, 30 + i) for i in range(2)]
+    one_by_one = [b.run(x) for b, x in zip(batches, q)]
+    n = Context.attn_prefix_paged_workspace_bytes(20, 1, 8, 2, 40, 1, 3500)
+    outs, streams = [torch.empty(q[0].shape, device=DEV) for _ in range(2)], [torch.cuda.Stream() for _ in range(2)]
+    args = [(dev32(b.pages), dev32(b.own), dev32(b.pre_pages), dev32(b.prefix), dev32(b.start), torch.empty(n, dtype=torch.uint8, device=DEV))
+            for b in batches]
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for b, x, o, s, (pages, own, pre, length, start, ws) in zip(batches, q, outs, streams, args):
+            with torch.cuda.stream(s):
+                f.ctx.attn_prefix_paged(x, o, *b.cache.all, pages, own, 40, pre, length, start, b.prefix[0], helpers.softmax_scale(), ws)
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(one_by_one, outs))
+
+
+def test_a_serving_run_with_a_common_prompt():
+    """A prompt appended once in two chunks, questions of three sequences behind it, single tokens: append, attention with the prefix, DeQuant."""
+    f, rng = fmt("general"), np.random.default_rng(17)
+    Hq, Hkv, B, P = 8, 2, 3, 150
+    table = paged_ref.cos_sin(400, 128)
+    rotary = Rotary(torch.from_numpy(table).to(DEV))
+    pages = paged_ref.page_table(rng, 14, [P] + [120] * B)
+    cache = paged_ref.Cache(f, Hkv, 14)
+    prompt, lens, seen = [], 0, [[[], []] for _ in range(B)]
+    for m in (100, 50):
+        lens += m
+        xk, xv = rows(rng, m, Hkv, torch.bfloat16)
+        f.ctx.append_paged(xk, xv, dev32([0, m]), dev32([lens]), *cache.all, dev32(pages[:1]), rotary=rotary)
+        prompt.append((paged_ref.rotate(f64(xk), np.arange(lens - m, lens), table, False), f64(xv)))
+    held = [f.decode(f.encode(np.concatenate([c[kind] for c in prompt])[:, h])) for kind in (0, 1) for h in range(Hkv)]
+    out = [torch.empty(P, Hkv, 128, device=DEV) for _ in range(2)]
+    f.ctx.decode_paged(*cache.all, dev32(pages[:1]), dev32([0, P]), dev32([P]), *out)
+    assert all(helpers.rel_l2(f64(out[kind][:, h]), held[kind * Hkv + h]) <= 1e-3 for kind in (0, 1) for h in range(Hkv))
+    own = [0] * B
+    for new in ([30, 1, 64], [1, 1, 1], [1, 1, 1]):
+        own = [a + b for a, b in zip(own, new)]
+        xk, xv = rows(rng, sum(new), Hkv, torch.bfloat16, extra=Hq)
+        at = np.concatenate([np.arange(P + n - m, P + n) for n, m in zip(own, new)])
+        f.ctx.append_paged(xk, xv, dev32(np.cumsum([0] + new)), dev32(own), *cache.all, dev32(pages[1:]), rotary=rotary, positions=dev32(at))
+        k, v, row = paged_ref.rotate(f64(xk), at, table, False), f64(xv), 0
+        for b, m in enumerate(new):
+            seen[b][0].append(k[row : row + m])
+            seen[b][1].append(v[row : row + m])
+            row += m
+        q = queries(B, 1, Hq, own[0])
+        got = torch.empty(q.shape, device=DEV)
+        ws = torch.empty(Context.attn_prefix_paged_workspace_bytes(B, 1, Hq, Hkv, 120, 1, P), dtype=torch.uint8, device=DEV)
+        f.ctx.attn_prefix_paged(q, got, *cache.all, dev32(pages[1:]), dev32(own), 120, dev32(pages[:1]), dev32([P]), dev32([0, B]), P,
+                                helpers.softmax_scale(), ws, rotary=rotary)
+        torch.cuda.synchronize()
+        want = np.zeros(q.shape)
+        for b in range(B):
+            mine = [f.decode(f.encode(np.concatenate(seen[b][kind])[:, h])) for kind in (0, 1) for h in range(Hkv)]
+            keys, values = ([(lambda m, x=np.concatenate([held[kind * Hkv + h], mine[kind * Hkv + h]]): x) for h in range(Hkv)] for kind in (0, 1))
+            qb = paged_ref.rotate(f64(q)[b], np.array([P + own[b] - 1]), table, False)
+            want[b] = paged_ref.attention(qb, keys, values, helpers.softmax_scale(), 1)
+        check_rows(f64(got), want, [P + n for n in own])
