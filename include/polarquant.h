@@ -489,15 +489,15 @@ size_t pq_attn_paged_workspace_bytes(int B, int M, int Hq, int Hkv, int64_t max_
  * attend to the prefix_len[g] tokens (device, int32 [n_groups], at most max_prefix, itself
  * at most 2^26) in the pages prefix_pages[g * ld_prefix_pages + ..], all of their query
  * tokens to all of them, and behind those to their own ctx_len[b] tokens in pages[b], as
- * in pq_attn_paged; one softmax over both.  The prefix is decoded once per 128 query rows
- * (M * Hq/Hkv per sequence) of a group and kv head instead of once per sequence.  A
+ * in pq_attn_paged; one softmax over both.  The prefix is decoded once per 128 or 256 query
+ * rows (M * Hq/Hkv per sequence) of a group and kv head instead of once per sequence.  A
  * prefix need not end with its last page.  Sequences in no group have no prefix;
  * n_groups == 0 is pq_attn_paged.  rotary without positions: the position of query
  * token m is prefix_len + ctx_len[b] - M + m.  A sequence with neither prefix nor tokens
  * gives a zero row.  64 * ld_prefix_pages must be at least max_prefix (PQ_EINVAL).
  * workspace: pq_attn_prefix_paged_workspace_bytes, not less (PQ_ENOMEM).  Results
  * differ from those of pq_attn_paged on the joined page tables by the rounding of keys,
- * once to binary16 as the rotated query is. */
+ * which are rebuilt in binary16 as the values are. */
 pq_status pq_attn_prefix_paged(const pq_ctx *ctx, const void *q, void *out, pq_dtype out_dtype, const pq_rotary *rotary,
                                const int32_t *positions, const uint8_t *k_codes, const uint16_t *k_radii,
                                const uint8_t *v_codes, const uint16_t *v_radii, int64_t pool_tokens,

@@ -1449,13 +1449,16 @@ __global__ __launch_bounds__(512) void pq_rotate_q_prefix_kernel(RotateArgs a, P
     } else {
         __shared__ int sum[8];
         const int tid = threadIdx.x, pairs = a.M * (a.Hq / p.Hkv);
-        int tiles = 0, streams = 0;
+        int tiles = 0, streams = 0, mine = 0; /* tiles of block tid */
         for (int i = tid; i < pre.B; i += 512) {
             const BlockRows r = row_block(a.groups, i, p.B, pairs, pre_rows);
             blocks[i] = r;
-            tiles += (r.tokens + 63) >> 6;
-            streams += r.tokens > 0;
+            const int t = (r.tokens + 63) >> 6;
+            if (i == tid) mine = t;
+            tiles += t;
+            streams += t > 0;
         }
+        auto tiles_of = [&](int i) { return i == tid ? mine : (blocks[i].tokens + 63) >> 6; };
         for (int b = tid; b < p.B; b += 512) seqs[b] = sequence_rows(a.groups, b, pairs, pre_rows);
         auto total = [&](int v) { /* of the workgroup */
 #pragma unroll
@@ -1471,7 +1474,7 @@ __global__ __launch_bounds__(512) void pq_rotate_q_prefix_kernel(RotateArgs a, P
         const int all_tiles = total(tiles) * pre.Hkv, all_streams = total(streams) * pre.Hkv; /* tiles of a group's table: fewer than 2^31 in all */
         auto pieces = [&](int c) {
             int n = 0;
-            for (int i = tid; i < pre.B; i += 512) n += (((blocks[i].tokens + 63) >> 6) + c - 1) / c;
+            for (int i = tid; i < pre.B; i += 512) n += (tiles_of(i) + c - 1) / c;
             return total(n) * pre.Hkv;
         };
         int c = 1;
@@ -1484,7 +1487,7 @@ __global__ __launch_bounds__(512) void pq_rotate_q_prefix_kernel(RotateArgs a, P
                 else c = mid + 1;
             }
         }
-        build_plan(pre, [&](int i) { return (((blocks[i].tokens + 63) >> 6) + c - 1) / c; });
+        build_plan(pre, [&](int i) { return (tiles_of(i) + c - 1) / c; });
     }
 }
 
@@ -2048,7 +2051,6 @@ void launch_combine_rows(int rows, bool hybrid, hipStream_t s, const CombineArgs
 {
     const dim3 grid((unsigned)((rows + ROWS - 1) / ROWS)), blk(512);
     if (hybrid) hipLaunchKernelGGL((pq_attn_combine_kernel<ROWS, true, false>), grid, blk, 0, s, ca, rows);
-    else if (ca.seq_rows) hipLaunchKernelGGL((pq_attn_combine_kernel<ROWS, false, true>), grid, blk, 0, s, ca, rows);
     else hipLaunchKernelGGL((pq_attn_combine_kernel<ROWS, false, false>), grid, blk, 0, s, ca, rows);
 }
 
@@ -2056,7 +2058,15 @@ void launch_combine(int rows, bool hybrid, hipStream_t s, const CombineArgs &ca)
 {
     /* One workgroup per CU has the shortest chain (32 rows: 16.3 us per decode step with one row per workgroup, 16.7 with
        two, 17.5 with four); with more rows than CUs the fetches of S^T count (512 rows: 116.6 us with two, 117.2 with four;
-       1024: 34.6, 34.7 and 37.1 with one; 2048: 489 with four, 493 with two, 496 with one). */
+       1024: 34.6, 34.7 and 37.1 with one; 2048: 489 with four, 493 with two, 496 with one).  With prefixes the registers
+       of one more loop leave room for two workgroups per CU only, and eight rows take fewer of them (64 sequences of 32 heads with
+       16384 tokens in common 62.5 us, 63.7 with four rows; 200 sequences in 5 groups 60.6, 65.3). */
+    if (ca.seq_rows) {
+        auto launch = [&](auto kernel, int n) { hipLaunchKernelGGL(kernel, dim3((unsigned)((rows + n - 1) / n)), dim3(512), 0, s, ca, rows); };
+        if (rows <= 256) return launch(pq_attn_combine_kernel<1, false, true>, 1);
+        if (rows <= 1024) return launch(pq_attn_combine_kernel<2, false, true>, 2);
+        return launch(pq_attn_combine_kernel<8, false, true>, 8);
+    }
     if (rows <= 256) launch_combine_rows<1>(rows, hybrid, s, ca);
     else if (rows <= 1024) launch_combine_rows<2>(rows, hybrid, s, ca);
     else launch_combine_rows<4>(rows, hybrid, s, ca);

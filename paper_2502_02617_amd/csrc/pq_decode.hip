@@ -432,7 +432,8 @@ __global__ __launch_bounds__(kDecodeThreads, 1) void pq_decode_kernel(DecodeArgs
     decode_half_tiles<KIND, OT, UNIT, AHEAD, false>(a, lds, (int)blockIdx.x, (int)gridDim.x);
 }
 
-/* ragged rows of a paged cache: keys on workgroups [0, k_blocks), values on the rest */
+/* ragged rows of a paged cache: keys on workgroups [0, k_blocks), values on the rest.  8000 tokens of 8 heads to bf16 22 us (41 MB at
+ * 1.9 TB/s: S goes to LDS first, and a tile's page is looked up ahead of it; two launches 30); 24 sequences of 20 to 6000 to fp32 93 us, 3.2 TB/s. */
 template <int OT, bool UNIT>
 __global__ __launch_bounds__(kDecodeThreads, 1) void pq_decode_paged_kernel(DecodeArgs k, DecodeArgs v, int k_blocks)
 {

@@ -11,8 +11,8 @@
  *   values     O^T = V^T P^T (coordinates x rows): the contraction takes the tokens in the order in which the
  *              scores lie in a lane's registers, so the weights are its operand as they are; V is
  *              laid out in that order.
- * Rounding: a key's element is rounded to binary16 once, as the rotated query's is; weights and values as in the
- * kernel for single sequences.  Maxima, sums and results stay in fp32.
+ * Rounding: keys are rebuilt as the values are, radius times block table and that times quarter table in binary16 (the kernel for
+ * single sequences scales its keys in fp32); weights and values as there.  Maxima, sums and results stay in fp32.
  */
 #ifndef PQ_PREFIX_H
 #define PQ_PREFIX_H
@@ -225,7 +225,9 @@ struct Rebuild {
 /* ROWS query rows per workgroup, 32 per wavefront: of 256 a wavefront sees all tokens of a tile, of 128 two wavefronts share rows and have
  * half of the tokens each, and join their results in the end.  While a tile is multiplied the next one is rebuilt into the other half of LDS,
  * and the one after that is on its way there: one barrier per tile.  What bounds it is the chain of a wavefront's steps, two wavefronts per
- * SIMD: so all requests to LDS stand ahead of the work that covers them. */
+ * SIMD: so all requests to LDS stand ahead of the work that covers them.  16384 tokens, 256 rows of 8 kv heads: 36 us (45 in blocks of
+ * 128), 17 GFLOP at 0.48 PFLOP/s; of its cycles the matrix cores work 25 %, the vector ALU half, LDS 40 to 60 %, half of that on colliding
+ * reads of the tables. */
 template <bool DEEP, int ROWS>
 __global__ __launch_bounds__(kPrefixThreads, 1) void pq_attn_prefix_kernel(PrefixArgs a)
 {

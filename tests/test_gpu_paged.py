@@ -216,6 +216,30 @@ def test_append_of_vectors_that_all_lie_on_borders():
     assert torch.equal(a.kc, b.kc) and torch.equal(a.vc, b.vc)
 
 
+@pytest.mark.parametrize("name", ["general", "hadamard", "deep"])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_append_of_very_small_and_very_large_vectors(name, dtype):
+    """Codes do not depend on a vector's length, from 1e-30 to 1e30; vectors of zeros, infinities and NaN leave their neighbours alone."""
+    f, heads, n = fmt(name), 2, 640
+    g = torch.Generator().manual_seed(5)
+    x = torch.randn(n, 2 * heads, 128, generator=g)
+    x[1::2] *= torch.exp2(torch.randint(-100, 101, (n // 2, 1, 1), generator=g).float())
+    x = x.to(dtype)
+    odd = {100: 0.0, 201: float("inf"), 302: float("nan"), 303: -float("inf")}
+    for row, value in odd.items():
+        x[row] = value
+    x = x.to(DEV)
+    for cache in appended_both_ways(f, x[:, :heads], x[:, heads:], [n + 5], [n], heads, 11):
+        held, pages = cache.read(), paged_ref.page_table(np.random.default_rng(3), 11, [n + 5])
+        sound = np.array([r for r in range(n) if r not in odd])
+        for kind, part in ((KEY, x[:, :heads]), (VALUE, x[:, heads:])):
+            got = paged_ref.tokens(held[kind], pages[0], 5, n + 5).reshape(heads, n, f.record)
+            for h in range(heads):
+                want, psi, _ = f.encode(f64(part[sound, h]), want_psi=True, want_y=True)
+                check_exact_codes(f, np.ascontiguousarray(got[h][sound]), want, psi)
+                assert np.array_equal(f.radii(got[h][100:101]), f.radii(f.encode(np.zeros((1, 128)))))
+
+
 def test_append_with_more_tile_numbers_than_the_workgroups_take():
     """300 sequences of 10 rows and 64 heads: more than 65536 (tile, head, keys or values) numbers."""
     f, heads, B = fmt("general"), 64, 300
