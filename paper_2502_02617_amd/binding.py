@@ -611,7 +611,7 @@ class Context:
         _check(library().pq_attn_paged(
             self._h, q.data_ptr(), out.data_ptr(), _dtype_code(out), ctypes.addressof(rotary) if rotary is not None else None,
             self._query_positions(positions, B, M), k_codes.data_ptr(), k_radii.data_ptr(), v_codes.data_ptr(), v_radii.data_ptr(),
-            pool_tokens, table, ld, _ints("ctx_len", ctx_len, B), B, M, Hq, heads, max_ctx, softmax_scale,
+            pool_tokens, table, ld, _ints("ctx_len", ctx_len, B), B, M, Hq, heads, int(max_ctx), float(softmax_scale),
             workspace.data_ptr(), workspace.numel() * workspace.element_size(), _stream()))
 
     def attn_prefix_paged(self, q, out, k_codes, k_radii, v_codes, v_radii, pages, ctx_len, max_ctx, prefix_pages, prefix_len, group_start,
@@ -626,9 +626,9 @@ class Context:
         _check(library().pq_attn_prefix_paged(
             self._h, q.data_ptr(), out.data_ptr(), _dtype_code(out), ctypes.addressof(rotary) if rotary is not None else None,
             self._query_positions(positions, B, M), k_codes.data_ptr(), k_radii.data_ptr(), v_codes.data_ptr(), v_radii.data_ptr(),
-            pool_tokens, table, ld, _ints("ctx_len", ctx_len, B), B, M, Hq, heads, max_ctx, pre_table, pre_ld,
-            _ints("prefix_len", prefix_len, n_groups), _ints("group_start", group_start, n_groups + 1), n_groups, max_prefix,
-            softmax_scale, workspace.data_ptr(), workspace.numel() * workspace.element_size(), _stream()))
+            pool_tokens, table, ld, _ints("ctx_len", ctx_len, B), B, M, Hq, heads, int(max_ctx), pre_table, pre_ld,
+            _ints("prefix_len", prefix_len, n_groups), _ints("group_start", group_start, n_groups + 1), n_groups, int(max_prefix),
+            float(softmax_scale), workspace.data_ptr(), workspace.numel() * workspace.element_size(), _stream()))
 
     @staticmethod
     def attn_prefix_paged_workspace_bytes(B, M, Hq, Hkv, max_ctx, n_groups, max_prefix):

@@ -266,3 +266,30 @@ def test_a_serving_run_with_a_common_prompt():
             qb = paged_ref.rotate(f64(q)[b], np.array([P + own[b] - 1]), table, False)
             want[b] = paged_ref.attention(qb, keys, values, helpers.softmax_scale(), 1)
         check_rows(f64(got), want, [P + n for n in own])
+
+
+def test_pages_whose_bytes_lie_beyond_32_bits():
+    """A head plane of 4.4 GB: the same calls on pages at its ends and on a pool of eight pages give the same bits."""
+    f, rng = fmt("general"), np.random.default_rng(23)
+    n_pages, Hq, lens = 1_500_000, 4, [190, 64, 130]
+    small = paged_ref.page_table(rng, 8, lens)
+    names = np.array([n_pages - 1, 0, 1_458_889, 7, n_pages - 2, 1_458_888, 1_459_000, 1])  # 1458888 * 2944 is just below 2^32
+    large = np.where(small >= 0, names[small], -1)
+    xk, xv = rows(rng, sum(lens), 1, torch.bfloat16)
+    q = queries(2, 1, Hq, 23)
+    results = []
+    for table, pool in ((small, 8), (large, n_pages)):
+        cache = paged_ref.Cache(f, 1, pool)
+        f.ctx.append_paged(xk, xv, dev32(np.cumsum([0] + lens)), dev32(lens), *cache.all, dev32(table))
+        f.ctx.append_paged(xk[:3], xv[:3], dev32([0, 1, 2, 3]), dev32([n - 5 for n in lens]), *cache.all, dev32(table))
+        out = [torch.zeros(sum(lens), 1, 128, device=DEV) for _ in range(2)]
+        f.ctx.decode_paged(*cache.all, dev32(table), dev32(np.cumsum([0] + lens)), dev32(lens), *out)
+        plain, shared = torch.zeros(q.shape, device=DEV), torch.zeros(q.shape, device=DEV)
+        ws = torch.empty(Context.attn_prefix_paged_workspace_bytes(2, 1, Hq, 1, 190, 1, 130), dtype=torch.uint8, device=DEV)
+        f.ctx.attn_paged(q, plain, *cache.all, dev32(table[:2]), dev32(lens[:2]), 190, helpers.softmax_scale(), ws)
+        f.ctx.attn_prefix_paged(q, shared, *cache.all, dev32(table[:2]), dev32(lens[:2]), 190, dev32(table[2:]), dev32(lens[2:]), dev32([0, 2]), 130,
+                                helpers.softmax_scale(), ws)
+        torch.cuda.synchronize()
+        results.append(out + [plain, shared])
+        del cache
+    assert all(torch.equal(a, b) for a, b in zip(*results)) and all(bool(torch.isfinite(a).all()) and bool(a.any()) for a in results[0])
