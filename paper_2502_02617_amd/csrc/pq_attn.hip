@@ -1424,27 +1424,30 @@ __device__ __forceinline__ void build_plan(const PlanArgs &a)
     });
 }
 
-/* workgroups [0, row_blocks) rotate kRotateRows query rows each, the last workgroup builds the work plan */
+/* the first workgroup builds the work plan, the others rotate kRotateRows query rows each */
 template <bool ROT>
-__global__ __launch_bounds__(512) void pq_rotate_q_kernel(RotateArgs a, PlanArgs p, int rows, int row_blocks)
+__global__ __launch_bounds__(512) void pq_rotate_q_kernel(RotateArgs a, PlanArgs p, int rows)
 {
-    if ((int)blockIdx.x < row_blocks) rotate_query_rows<ROT>(a, kRotateRows * (int)blockIdx.x, rows);
-    else build_plan(p);
+    if (blockIdx.x == 0) build_plan(p);
+    else rotate_query_rows<ROT>(a, kRotateRows * ((int)blockIdx.x - 1), rows);
 }
 
 #include "pq_prefix.h"
 
-/* First launch of attention with prefixes: as above, and one more workgroup builds the plan of the groups' row blocks and leaves the
- * blocks and every sequence's place in them.  The plan counts pieces, not tiles: a stream of T tiles is cut into ceil(T / c) of them with the
+/* First launch of attention with prefixes: the rotation, the plan as above, a workgroup that leaves every sequence's place in the groups'
+ * row blocks, and one for these blocks and their plan.  The plan counts pieces, not tiles: a stream of T tiles is cut into ceil(T / c) of them with the
  * smallest c for which there is one for a workgroup at most, so that none goes on into the next stream, whose start and end would cost a
  * workgroup another 6 us, three tiles' time (6 groups, 50 sequences: 27 -> 23 us).  With more streams than workgroups c is 1. */
 template <bool ROT>
 __global__ __launch_bounds__(512) void pq_rotate_q_prefix_kernel(RotateArgs a, PlanArgs p, PlanArgs pre, BlockRows *blocks, SequenceRows *seqs, int rows,
-                                                                 int row_blocks, int pre_rows)
+                                                                 int pre_rows)
 {
-    if ((int)blockIdx.x < row_blocks) {
-        rotate_query_rows<ROT>(a, kRotateRows * (int)blockIdx.x, rows);
-    } else if ((int)blockIdx.x == row_blocks) {
+    const int block = (int)blockIdx.x - 3; /* the longest chain first */
+    if (block >= 0) {
+        rotate_query_rows<ROT>(a, kRotateRows * block, rows);
+    } else if (block == -1) {
+        for (int b = threadIdx.x; b < p.B; b += 512) seqs[b] = sequence_rows(a.groups, b, a.M * (a.Hq / p.Hkv), pre_rows);
+    } else if (block == -2) {
         build_plan(p);
     } else {
         __shared__ int sum[8];
@@ -1459,7 +1462,6 @@ __global__ __launch_bounds__(512) void pq_rotate_q_prefix_kernel(RotateArgs a, P
             streams += t > 0;
         }
         auto tiles_of = [&](int i) { return i == tid ? mine : (blocks[i].tokens + 63) >> 6; };
-        for (int b = tid; b < p.B; b += 512) seqs[b] = sequence_rows(a.groups, b, pairs, pre_rows);
         auto total = [&](int v) { /* of the workgroup */
 #pragma unroll
             for (int d = 32; d >= 1; d >>= 1) v += __shfl_xor(v, d);
@@ -2170,11 +2172,11 @@ pq_status attention_launches(const pq_ctx *ctx, const StepAppend *app, const Ste
         else hipLaunchKernelGGL(pq_rotate_window_kernel<1>, grid, blk, 0, s, ra, pa, rows, row_blocks, wa, (int)wblocks);
     } else if (pre) {
         const PlanArgs pb{nullptr, nullptr, pp.n_blocks, Hkv, 0, 0, pp.slots, pre_plan};
-        auto rotate = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((unsigned)row_blocks + 2u), dim3(512), 0, s, ra, pa, pb, pre_blocks, seq_rows, rows, row_blocks, pp.rows); };
+        auto rotate = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((unsigned)row_blocks + 3u), dim3(512), 0, s, ra, pa, pb, pre_blocks, seq_rows, rows, pp.rows); };
         if (ra.rot.cs) rotate(pq_rotate_q_prefix_kernel<true>);
         else rotate(pq_rotate_q_prefix_kernel<false>);
     } else {
-        auto rotate = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((unsigned)row_blocks + 1u), dim3(512), 0, s, ra, pa, rows, row_blocks); };
+        auto rotate = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((unsigned)row_blocks + 1u), dim3(512), 0, s, ra, pa, rows); };
         if (ra.rot.cs) rotate(pq_rotate_q_kernel<true>);
         else rotate(pq_rotate_q_kernel<false>);
     }
