@@ -218,37 +218,51 @@ __device__ __forceinline__ double element_exact(const AppendPagedArgs &a, int ki
     return x;
 }
 
-/* NV vectors (row, head) of kind KIND by one workgroup of 512 threads, vec0 .. vec0 + NV - 1 as far as they are below n_vec; wavefronts
- * 2 r and 2 r + 1 fetch vector r, the first of them runs its recursion. */
+/* Vectors (row, head) of kind KIND, NV at a time, from NV * block on, with NV 8 in steps of 8 * n_blocks: S is fetched once for them all.  Two wavefronts
+ * fetch a vector (NV 8: one), the first of them runs its recursion. */
 template <int XT, int KIND, int NV>
-__device__ __forceinline__ void append_vectors_exact(const AppendPagedArgs &a, int64_t vec0, int64_t n_vec, ExactLds<NV> &lds)
+__device__ __forceinline__ void append_vectors_exact(const AppendPagedArgs &a, int block, int n_blocks, int64_t n_vec, ExactLds<NV> &lds)
 {
+    constexpr int kWaves = NV == 8 ? 1 : 2;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     ExactSlice s;
     s.load(a.exact->S, tid);
     ExactBounds bounds;
     bounds.load(*a.exact, *a.consts);
-    const int r = min(wave >> 1, NV - 1); /* a vector beyond the range repeats the last one and is not written */
-    const int64_t vec = min(vec0 + r, n_vec - 1), row = vec / a.n_heads;
-    const int head = (int)(vec - row * a.n_heads);
-    const PagedPlace at = paged_place(a, row, lane);
-    if ((wave >> 1) < NV)
-        lds.x[r][tid & 127] = element_exact<XT>(a, KIND, row * a.ld_token + (int64_t)head * a.ld_head, at.position, tid & 127);
-    __syncthreads();
-    multiply_exact<NV>(s, lds, tid);
-    __syncthreads();
-    if ((wave & 1) == 0 && (wave >> 1) < NV && vec0 + r < n_vec && at.page >= 0)
-        write_exact<KIND>(a, bounds, rotated_exact(lds, r, 2 * lane), rotated_exact(lds, r, 2 * lane + 1), head * a.table.pool_pages + at.page, at.tau, lane);
+    const int r = min(wave / kWaves, NV - 1); /* a vector beyond the range repeats the last one and is not written */
+    const bool mine = wave / kWaves < NV;
+    for (int64_t vec0 = (int64_t)NV * block; vec0 < n_vec; vec0 += (int64_t)NV * n_blocks) {
+        const int64_t vec = min(vec0 + r, n_vec - 1), row = vec / a.n_heads;
+        const int head = (int)(vec - row * a.n_heads);
+        int l = lane; /* what follows from the lane is formed here: kept over the loop it takes the second workgroup's registers */
+        asm volatile("" : "+v"(l));
+        const PagedPlace at = paged_place(a, row, l);
+        if (mine) {
+            const int64_t off = row * a.ld_token + (int64_t)head * a.ld_head;
+#pragma unroll
+            for (int i = 0; i < 2 / kWaves; ++i) {
+                const int c = l + 64 * (kWaves == 1 ? i : wave & 1);
+                lds.x[r][c] = element_exact<XT>(a, KIND, off, at.position, c);
+            }
+        }
+        __syncthreads();
+        multiply_exact<NV>(s, lds, tid);
+        __syncthreads();
+        if (wave % kWaves == 0 && mine && vec0 + r < n_vec && at.page >= 0)
+            write_exact<KIND>(a, bounds, rotated_exact(lds, r, 2 * l), rotated_exact(lds, r, 2 * l + 1), head * a.table.pool_pages + at.page, at.tau, l);
+        if (NV < 8) return; /* a workgroup for every NV of them */
+        /* the next vectors' coordinates go where nobody reads any more, their products behind the next barrier */
+    }
 }
 
 /* workgroups [0, n_blocks): keys, the rest: values */
 template <int XT, int NV>
-__global__ __launch_bounds__(512) void pq_append_paged_kernel(AppendPagedArgs a, int64_t n_vec, int n_blocks)
+__global__ __launch_bounds__(512, NV == 8 ? 4 : 1) void pq_append_paged_kernel(AppendPagedArgs a, int64_t n_vec, int n_blocks)
 {
     __shared__ ExactLds<NV> lds;
     const int blk = (int)blockIdx.x;
-    if (blk < n_blocks) append_vectors_exact<XT, PQ_KEY, NV>(a, (int64_t)NV * blk, n_vec, lds);
-    else append_vectors_exact<XT, PQ_VALUE, NV>(a, (int64_t)NV * (blk - n_blocks), n_vec, lds);
+    if (blk < n_blocks) append_vectors_exact<XT, PQ_KEY, NV>(a, blk, n_blocks, n_vec, lds);
+    else append_vectors_exact<XT, PQ_VALUE, NV>(a, blk - n_blocks, n_blocks, n_vec, lds);
 }
 
 /* ---- whole tiles: chunks of prompts ----
@@ -789,22 +803,30 @@ extern "C" pq_status pq_append_paged(const pq_ctx *ctx, const void *xk, const vo
                       pq_rotary_args(rotary), positions, ds->exact, ds->consts};
     const int64_t n_vec = n_rows * n_heads;
     hipStream_t s = static_cast<hipStream_t>(hip_stream);
-    /* Whole tiles or vectors one by one: a vector takes 4.1 ns beyond the first few hundred (S, 128 KB, is fetched for every four), a tile that
-       is written in part 15 ns and one number of a tile for every sequence whether it has tokens in it or not, the first of them 6 us more
-       (heads x sequences x tokens each, us, vectors / tiles: 8 x 1 x 128 14.1 / 14.1, 512 40 / 14; 8 x 64 x 4 24 / 43, 8 39 / 43, 16 72 / 46; 8 x 256 x 1
-       25 / 71, 8 142 / 142; 8 x 16 x 16 24 / 21). */
-    if (n_rows >= 8 * (int64_t)n_seq + 768 / n_heads) {
+    /* Whole tiles or vectors one by one: a vector takes 2.6 ns beyond the first two thousand, a tile that is written in part 17 ns
+       and one number of a tile for every sequence whether it has tokens in it or not, the first of them 6 us more (heads x sequences x tokens
+       each, us, vectors / tiles: 8 x 1 x 128 14.6 / 15.2, 256 21 / 14; 8 x 64 x 8 32 / 43, 16 50 / 45; 8 x 256 x 8 88 / 140, 16 167 / 156;
+       2 x 64 x 8 14.5 / 16.6, 16 21 / 18; 2 x 1 x 256 11.3 / 13.4). */
+    if (n_rows >= 12 * (int64_t)n_seq + 1024 / n_heads) {
         if (xt == PQ_BF16) launch_chunks<PQ_BF16>(ctx, ds, a, s);
         else launch_chunks<PQ_F32>(ctx, ds, a, s);
         PQ_HIP_TRY(hipGetLastError());
         return PQ_OK;
     }
-    const int nv = append_vectors_per_block(2 * n_vec);
-    const int n_blocks = (int)((n_vec + nv - 1) / nv);
+    /* more than two workgroups per CU take four at a time: eight, and S stays in registers from the first to the last of them (8 x 64 x 8: 39 us
+       with S fetched for every four, 32 so; 8 x 64 x 16 72 and 50; 8 x 256 x 1 25 and 19) */
+    const int nv = n_vec > 4 * 256 ? 8 : append_vectors_per_block(2 * n_vec);
+    const int n_blocks = (int)min((n_vec + nv - 1) / nv, (int64_t)256); /* two workgroups per CU, keys and values; 128 registers allow them */
     const dim3 grid(2u * (unsigned)n_blocks), block(512);
     auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, s, a, n_vec, n_blocks); };
-    if (xt == PQ_BF16) nv == 1 ? launch(pq_append_paged_kernel<PQ_BF16, 1>) : launch(pq_append_paged_kernel<PQ_BF16, 4>);
-    else nv == 1 ? launch(pq_append_paged_kernel<PQ_F32, 1>) : launch(pq_append_paged_kernel<PQ_F32, 4>);
+    auto with = [&](auto type) {
+        constexpr int XT = decltype(type)::value;
+        if (nv == 1) launch(pq_append_paged_kernel<XT, 1>);
+        else if (nv == 4) launch(pq_append_paged_kernel<XT, 4>);
+        else launch(pq_append_paged_kernel<XT, 8>);
+    };
+    if (xt == PQ_BF16) with(std::integral_constant<int, PQ_BF16>{});
+    else with(std::integral_constant<int, PQ_F32>{});
     PQ_HIP_TRY(hipGetLastError());
     return PQ_OK;
 }
