@@ -216,6 +216,15 @@ def test_append_of_vectors_that_all_lie_on_borders():
     assert torch.equal(a.kc, b.kc) and torch.equal(a.vc, b.vc)
 
 
+@pytest.mark.parametrize("heads,n", [(1, 1031), (3, 683), (1, 4099)])
+def test_append_of_single_rows_in_several_rounds(heads, n):
+    """More rows of their own than one round of the workgroups takes, and a last round in part."""
+    f = fmt("general")
+    xk, xv = rows(np.random.default_rng(n), n, heads, torch.bfloat16)
+    a, b = appended_both_ways(f, xk, xv, [n + 5], [n], heads, (n + 68) // 64)
+    assert torch.equal(a.kc, b.kc) and torch.equal(a.vc, b.vc) and bool((a.vc != 0).any())
+
+
 @pytest.mark.parametrize("name", ["general", "hadamard", "deep"])
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
 def test_append_of_very_small_and_very_large_vectors(name, dtype):
@@ -241,11 +250,11 @@ def test_append_of_very_small_and_very_large_vectors(name, dtype):
 
 
 def test_append_with_more_tile_numbers_than_the_workgroups_take():
-    """300 sequences of 10 rows and 64 heads: more than 65536 (tile, head, keys or values) numbers."""
+    """300 sequences of 14 rows and 64 heads: more than 65536 (tile, head, keys or values) numbers."""
     f, heads, B = fmt("general"), 64, 300
-    lens, new = [(3 * i) % 100 + 10 for i in range(B)], [10] * B
+    lens, new = [(3 * i) % 100 + 14 for i in range(B)], [14] * B
     n_pages = sum((n + 63) // 64 for n in lens)
-    xk, xv = rows(np.random.default_rng(2), 10 * B, heads, torch.bfloat16)
+    xk, xv = rows(np.random.default_rng(2), 14 * B, heads, torch.bfloat16)
     a, b = appended_both_ways(f, xk, xv, lens, new, heads, n_pages)
     assert torch.equal(a.kc, b.kc) and torch.equal(a.vc, b.vc)
     assert bool((a.kc != 0).any())
